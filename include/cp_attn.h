@@ -68,6 +68,8 @@ extern "C" {
 #define CP_KV_BLOCK_TOKENS 16
 #define CP_MAX_MERGE_PARTS 16
 #define CP_MAX_DEGREE 64        /* largest CP degree C of any call */
+#define CP_KV_MAX_CACHES 256    /* caches (K or V of a layer) of one call on pages */
+#define CP_KV_MAX_LIST 4096     /* sequences of one call on pages */
 #define CP_NOALLOC_SCRATCH_BYTES (32u << 20) /* device scratch of cp_attn_partial_noalloc, per GPU */
 
 /* kv_rank values of cp_partial_desc besides a rank number 0..C-1. */
@@ -416,6 +418,216 @@ int cp_repartition_all(int64_t P, int64_t R, int32_t C_src, const void* const* s
 int cp_kv_gather(const void* k_cache, const void* v_cache, int64_t n_blocks, const int32_t* block_table,
                  int64_t table_len, int64_t pos_begin, int64_t n_tokens, int32_t n_heads_kv,
                  int32_t head_dim, void* k_rows, void* v_rows, void* stream);
+
+/* ---------------------------------------------------------------------- */
+/* Attention over a paged cache, and through a sliding window             */
+
+/*
+ * A batch of sequences in a paged cache, as the calls below take it.  The
+ * arrays of integers are device memory, read by the kernels when they run: a
+ * captured launch follows lengths and tables that change between replays.
+ *   k_cache, v_cache  bf16 [n_blocks][16][n_heads_kv][128], 16-byte aligned.
+ *   tables      int32 [n_seqs][table_stride]: the page of each 16 positions of
+ *               a sequence.  An entry outside [0, n_blocks), and any position
+ *               beyond 16 * table_stride, names no page: its keys and values
+ *               read as zeros, and nothing is written through it.
+ *   kv_len      int32 [n_seqs]: the positions of a sequence, its new tokens
+ *               included (below 0 acts as 0, above 2^30 as 2^30).
+ * New tokens come as rows: with q_start (device int32 [n_seqs + 1], ascending),
+ * sequence s has rows q_start[s] .. q_start[s + 1] - 1 of n_rows; without
+ * (NULL) every sequence has n_rows / n_seqs.  The rows are the last positions of
+ * their sequence: row i of n is position kv_len[s] - n + i (one below 0 is none:
+ * it sees no key and is not stored in the cache).  Rows outside every sequence
+ * -- before q_start[0], from q_start[n_seqs] on -- are left as they were.
+ */
+typedef struct cp_paged_kv {
+  void* k_cache;
+  void* v_cache;
+  int64_t n_blocks;
+  const int32_t* tables;
+  int64_t table_stride;
+  const int32_t* kv_len;
+  int32_t n_seqs;
+  int32_t n_heads_kv;
+} cp_paged_kv;
+
+/*
+ * Sizing call of cp_attn_paged (a library utility, not from the paper): device
+ * bytes of its workspace for any contents of the device arrays; 0 on invalid
+ * arguments (cp_last_error says why).
+ */
+size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_q, int32_t n_heads_q,
+                                    int32_t n_heads_kv);
+
+/*
+ * Causal attention (Sec. 2.1) of every sequence's new rows over its positions in
+ * the paged cache, their own included (store them first: cp_kv_append): chunks
+ * of prompts behind any context (Sec. 2.2, without its block boundary), single
+ * tokens, or a mix of them in one launch.  Row at position p attends to
+ * the keys j <= p; with a window, to those with j > p - window or j < n_sink.
+ *   kv          host struct, read during the call only.
+ *   q           bf16 [n_rows][n_heads_q][128], rows q_stride elements apart (0:
+ *               dense; else a multiple of 8, at least n_heads_q * 128).
+ *   q_start     as above, or NULL (n_rows % n_seqs == 0).
+ *   max_q       the most rows of a sequence (ignored with q_start NULL).  Rows of
+ *               a sequence past it are left as they were.  Up to 64 (row, query
+ *               head) pairs per KV head take kernels for few rows.
+ *   n_heads_q   a multiple of n_heads_kv; head_dim 128.
+ *   softmax_scale  <= 0 selects 1/sqrt(head_dim).
+ *   window      keys visible behind a row, itself included; 0: all.
+ *   n_sink      first positions that stay visible behind the window, >= 0.
+ *   o           bf16 [n_rows][n_heads_q][128].
+ *   lse         fp32 [n_rows][n_heads_q], natural log; or NULL.
+ *   workspace   device, 256-byte aligned, of the size above; it holds partial
+ *               results while the call's kernels run: calls that may overlap
+ *               (other streams, graphs replayed side by side) need their own.
+ * A row that sees no key has O = 0, LSE = -inf; a NaN among its scores gives O =
+ * NaN, LSE = -inf.  Keys and values that a row does not see have no effect on
+ * it, whatever they hold.
+ * Errors: CP_ERR_INVALID (shapes, pointers, alignment, window or n_sink < 0),
+ * CP_ERR_UNSUPPORTED (head_dim; n_rows above 2^30, or times n_heads_q /
+ * n_heads_kv above 2^31 - 1), CP_ERR_CAPACITY (workspace), CP_ERR_HIP.
+ */
+int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_stride, int64_t n_rows, const int32_t* q_start,
+                  int64_t max_q, int32_t n_heads_q, int32_t head_dim, float softmax_scale, int64_t window,
+                  int64_t n_sink, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sizing call of cp_attn_window (a library utility, not from the paper), as
+ * cp_attn_paged_workspace_size.
+ */
+size_t cp_attn_window_workspace_size(const cp_rank_plan* plan, int32_t n_heads_q, int32_t n_heads_kv);
+
+/*
+ * A rank's zigzag rows (Sec. 2.1) through a sliding window: the row at position
+ * p attends to the keys j <= p with j > p - window or j < n_sink, of the cached
+ * prefix (paged, as in cp_partial_desc) and of the new tokens (all-gathered,
+ * original order).  Only the keys that some row sees are read.  (The window
+ * itself is not from the paper; window 0 is its causal attention.)
+ *   plan        from cp_shard_plan (checked against it).
+ *   q           bf16 [plan->n_rows][n_heads_q][128], local order.
+ *   k_new, v_new  bf16 [R][n_heads_kv][128].
+ *   k_cache, v_cache, n_blocks, block_table, table_len  the prefix: NULL and 0
+ *               allowed when P == 0; else P % 16 == 0 and table_len >= P / 16.
+ *               Entries outside [0, n_blocks) read as zeros.
+ *   window, n_sink, softmax_scale, workspace  as in cp_attn_paged.
+ *   o, lse      bf16 and fp32 (or NULL), in out_order as in cp_partial_desc.
+ * Errors: as cp_attn_paged, and a plan that is not cp_shard_plan's.
+ */
+int cp_attn_window(const cp_rank_plan* plan, const void* q, const void* k_new, const void* v_new, const void* k_cache,
+                   const void* v_cache, int64_t n_blocks, const int32_t* block_table, int64_t table_len,
+                   int32_t n_heads_q, int32_t n_heads_kv, int32_t head_dim, float softmax_scale, int64_t window,
+                   int64_t n_sink, void* o, float* lse, int32_t out_order, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/* ---------------------------------------------------------------------- */
+/* Pages of a cache                                                       */
+
+/*
+ * Stores a batch's new K and V rows at their positions in the paged cache (Sec.
+ * 2.2: prefill and decoding build the KV states of their tokens; Sec. 7.1, 8:
+ * cache blocks), at any position of a page, before cp_attn_paged reads them.
+ *   kv          as above; the caches are written.  head_dim any multiple of 8.
+ *   k_rows, v_rows  bf16, row r at r * k_stride (v_stride) elements, its
+ *               n_heads_kv * head_dim values dense: 0 for dense rows, else a
+ *               multiple of 8 and no less than that (a fused projection's output
+ *               is read where it lies).  16-byte aligned.
+ * The sequences' new positions must not share pages.
+ * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n_rows above 2^30), CP_ERR_HIP.
+ */
+int cp_kv_append(const cp_paged_kv* kv, const void* k_rows, const void* v_rows, int64_t k_stride, int64_t v_stride,
+                 int64_t n_rows, const int32_t* q_start, int32_t head_dim, void* stream);
+
+/*
+ * Page tables, lengths and reference counts of the sequences of one pool, in
+ * device memory (Sec. 7.1: cache blocks are shared by prefix; Sec. 8: blocks are
+ * reserved and released), which the calls below change:
+ *   tables      int32 [n_seqs][table_stride], -1 where a sequence has no page.
+ *   kv_len      int32 [n_seqs].
+ *   refs        int32 [n_blocks]: the table entries that name a page; 0: free.
+ * They keep refs what it says if it was, and give the lowest free pages first: the
+ * results do not depend on timing.  One call at a time may run on a pool.
+ * Sequence numbers outside [0, n_seqs) are passed over, and so is a sequence
+ * that a list names again; lists hold up to CP_KV_MAX_LIST entries.
+ * `missing` (device int32, 1; overwritten) is the number of entries of the
+ * list that got nothing.
+ */
+typedef struct cp_kv_pool {
+  int32_t* tables;
+  int64_t table_stride;
+  int32_t* kv_len;
+  int32_t* refs;
+  int64_t n_blocks;
+  int32_t n_seqs;
+  int32_t reserved; /* 0 */
+} cp_kv_pool;
+
+/*
+ * Copies pages: page dst[i] of every cache receives page src[i] (Sec. 7.2, 8:
+ * replicated KV states are installed in reserved blocks).  Pairs with a page
+ * outside [0, n_blocks) are passed over; no page may be the destination of two
+ * pairs, or of one and the source of another (its contents are then undefined).
+ *   caches      host array of n_caches device pointers (1..CP_KV_MAX_CACHES), each
+ *               [n_blocks][page_bytes], 16-byte aligned: K and V of every layer.
+ *   page_bytes  16 * n_heads_kv * head_dim * 2, a positive multiple of 16.
+ *   src, dst    device int32 [n], any n.
+ * Errors: CP_ERR_INVALID, CP_ERR_HIP.
+ */
+int cp_kv_copy_pages(void* const* caches, int32_t n_caches, int64_t n_blocks, int64_t page_bytes, const int32_t* src,
+                     const int32_t* dst, int64_t n, void* stream);
+
+/*
+ * Makes room for add[i] more tokens of sequence seqs[i]: raises its kv_len by
+ * that and gives it a page for every 16 positions that its length did not reach
+ * before (Sec. 8: blocks are reserved before KV states are installed).  The
+ * sequences are served in the order of the list until one asks for more pages
+ * than are left: it and those after it that need pages get nothing, as does one
+ * whose table is too short or whose add is negative, and keep their length.
+ * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
+ */
+int cp_kv_reserve(const cp_kv_pool* pool, const int32_t* seqs, const int32_t* add, int64_t n, int32_t* missing,
+                  void* stream);
+
+/*
+ * Sequence children[i] becomes a continuation of parents[i] (Sec. 7.1: requests
+ * share the blocks of a common prefix): it shares the pages that the parent
+ * has filled, receives a copy (in every cache) of a last page that is filled in
+ * part, and has the parent's length.  Its own table row is overwritten: a child
+ * must hold no pages (cp_kv_free).  A child that is also a parent in the list, or
+ * whose copy finds no free page, gets nothing: an empty row, length 0 (a
+ * parent of the list: unchanged).
+ *   caches, n_caches, page_bytes  as in cp_kv_copy_pages; n_caches may be 0.
+ * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
+ */
+int cp_kv_fork(const cp_kv_pool* pool, void* const* caches, int32_t n_caches, int64_t page_bytes,
+               const int32_t* parents, const int32_t* children, int64_t n, int32_t* missing, void* stream);
+
+/*
+ * Gives back the pages of sequence seqs[i] whose tokens all lie in [begin[i],
+ * end[i]): their entries become -1, and a page that no other table names is free
+ * (Sec. 8: blocks are released; behind a sliding window: begin = n_sink, end =
+ * kv_len - window).  The page that holds the last token is given back if end
+ * reaches kv_len; with begin <= 0 too the sequence is empty and its kv_len 0.
+ * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
+ */
+int cp_kv_free(const cp_kv_pool* pool, const int32_t* seqs, const int32_t* begin, const int32_t* end, int64_t n,
+               void* stream);
+
+/* Sizing call of cp_kv_compact (a library utility, not from the paper). */
+size_t cp_kv_compact_workspace_size(int64_t n_blocks);
+
+/*
+ * Moves the pages in use to the front of the pool (Sec. 6.2: after a worker
+ * split or merge its blocks are installed anew): of n pages in use the ones
+ * numbered n and above move, in ascending order, to the free ones below n, and
+ * every table entry and reference count follows.  Every sequence that names a
+ * page of the pool must be in the pool's tables.
+ *   caches, n_caches, page_bytes  as in cp_kv_fork.
+ *   workspace   device, 256-byte aligned, of the size above.
+ * Errors: CP_ERR_INVALID, CP_ERR_CAPACITY (workspace), CP_ERR_HIP.
+ */
+int cp_kv_compact(const cp_kv_pool* pool, void* const* caches, int32_t n_caches, int64_t page_bytes, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

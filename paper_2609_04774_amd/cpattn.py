@@ -30,12 +30,17 @@ CP_KV_NONE = -2
 CP_OUT_LOCAL = 0
 CP_OUT_SEQUENCE = 1
 CP_MAX_DEGREE = 64
+CP_KV_MAX_CACHES = 256
+CP_KV_MAX_LIST = 4096
 CP_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 EXPORTED = ("cp_status_string", "cp_last_error", "cp_shard_plan", "cp_shard_inverse",
             "cp_attn_partial_workspace_size", "cp_attn_partial", "cp_set_workgroup_rows",
             "cp_attn_partial_noalloc", "cp_attn_merge",
-            "cp_kv_writeback", "cp_repartition", "cp_repartition_all", "cp_kv_gather")
+            "cp_kv_writeback", "cp_repartition", "cp_repartition_all", "cp_kv_gather",
+            "cp_attn_paged_workspace_size", "cp_attn_paged", "cp_attn_window_workspace_size", "cp_attn_window",
+            "cp_kv_append", "cp_kv_copy_pages", "cp_kv_reserve", "cp_kv_fork", "cp_kv_free",
+            "cp_kv_compact_workspace_size", "cp_kv_compact")
 
 
 class CpChunk(ctypes.Structure):
@@ -70,6 +75,18 @@ class CpPartialDesc(ctypes.Structure):
                 ("o", ctypes.c_void_p), ("lse", ctypes.c_void_p),
                 ("n_blocks", ctypes.c_int64),
                 ("out_order", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class CpPagedKv(ctypes.Structure):
+    _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("n_blocks", ctypes.c_int64),
+                ("tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("n_heads_kv", ctypes.c_int32)]
+
+
+class CpKvPool(ctypes.Structure):
+    _fields_ = [("tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("n_blocks", ctypes.c_int64), ("n_seqs", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class CpError(RuntimeError):
@@ -130,6 +147,26 @@ def _load():
     lib.cp_kv_gather.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                  ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                  ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    i32, i64, size, ptr, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float
+    kv, pool, plan, ptrs = (ctypes.POINTER(t) for t in (CpPagedKv, CpKvPool, CpRankPlan, ctypes.c_void_p))
+    lib.cp_attn_paged_workspace_size.restype = size
+    lib.cp_attn_paged_workspace_size.argtypes = [i32, i64, i64, i32, i32]
+    lib.cp_attn_window_workspace_size.restype = size
+    lib.cp_attn_window_workspace_size.argtypes = [plan, i32, i32]
+    lib.cp_kv_compact_workspace_size.restype = size
+    lib.cp_kv_compact_workspace_size.argtypes = [i64]
+    for name, args in (
+            ("cp_attn_paged", [kv, ptr, i64, i64, ptr, i64, i32, i32, f32, i64, i64, ptr, ptr, ptr, size, ptr]),
+            ("cp_attn_window", [plan, ptr, ptr, ptr, ptr, ptr, i64, ptr, i64, i32, i32, i32, f32, i64, i64, ptr, ptr,
+                                i32, ptr, size, ptr]),
+            ("cp_kv_append", [kv, ptr, ptr, i64, i64, i64, ptr, i32, ptr]),
+            ("cp_kv_copy_pages", [ptrs, i32, i64, i64, ptr, ptr, i64, ptr]),
+            ("cp_kv_reserve", [pool, ptr, ptr, i64, ptr, ptr]),
+            ("cp_kv_fork", [pool, ptrs, i32, i64, ptr, ptr, i64, ptr, ptr]),
+            ("cp_kv_free", [pool, ptr, ptr, ptr, i64, ptr]),
+            ("cp_kv_compact", [pool, ptrs, i32, i64, ptr, size, ptr])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     return lib
 
 
@@ -461,3 +498,292 @@ def repartition_all(prefix_len: int, new_len: int, src_sets, dst_sets, stream=No
     row_bytes = math.prod(ref.shape[1:]) * ref.element_size()
     _check(lib.cp_repartition_all(prefix_len, new_len, C_src, srcs, C_dst, dsts, n_sets, row_bytes,
                                   _stream_handle(stream)))
+
+
+# --- attention over a paged cache -----------------------------------------------------
+
+def _same_device(device, named, stream=None):
+    """The calls below launch on the current device: every tensor, and the
+    stream if one is given, has to be there."""
+    import torch
+    here = torch.cuda.current_device()
+    if device.index != here:
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{here}")
+    for name, t in named:
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, expected {device}")
+
+
+def _rows_of(t, name: str, heads: int, D: int):
+    """Elements between the rows of a bf16 GPU tensor [rows, heads, D] whose
+    rows are dense (a slice of a fused projection's output is fine)."""
+    import torch
+    if t.dtype != torch.bfloat16 or not t.is_cuda:
+        _dev(t, name, torch.bfloat16)
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
+        raise ValueError(f"{name} must have shape [rows, {heads}, {D}], has {tuple(t.shape)}")
+    rows, _, _ = t.shape
+    stride = t.stride()
+    if rows and ((heads > 1 and stride[1] != D) or (D > 1 and stride[2] != 1) or
+                 (rows > 1 and (stride[0] < heads * D or stride[0] % 8))):
+        raise ValueError(f"the rows of {name} must be dense, and a multiple of 8 elements apart")
+    return stride[0] if rows > 1 else heads * D
+
+
+class PagedKV:
+    """A batch of sequences in a paged cache (cp_paged_kv): k_cache, v_cache
+    bf16 [blocks, 16, Hkv, D], tables int32 [n_seqs, pages] and kv_len int32
+    [n_seqs] on the GPU.  Made once for buffers that an engine keeps: their
+    contents may change between calls."""
+
+    def __init__(self, k_cache, v_cache, tables, kv_len):
+        import torch
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+            _dev(t, name, torch.bfloat16)
+            if t.dim() != 4 or t.shape[1] != CP_KV_BLOCK_TOKENS:
+                raise ValueError(f"{name} must have shape [blocks, 16, heads, D], has {tuple(t.shape)}")
+        if k_cache.shape != v_cache.shape:
+            raise ValueError("k_cache and v_cache differ in shape")
+        _dev(tables, "tables", torch.int32)
+        if tables.dim() != 2:
+            raise ValueError("tables must have shape [n_seqs, pages]")
+        _dev(kv_len, "kv_len", torch.int32, tables.shape[0])
+        if kv_len.dim() != 1:
+            raise ValueError("kv_len must have shape [n_seqs]")
+        self.device = k_cache.device
+        for name, t in (("v_cache", v_cache), ("tables", tables), ("kv_len", kv_len)):
+            if t.device != self.device:
+                raise ValueError(f"{name} is on {t.device}, k_cache on {self.device}")
+        self.n_seqs, self.n_heads, self.head_dim = tables.shape[0], k_cache.shape[2], k_cache.shape[3]
+        self.tensors = (k_cache, v_cache, tables, kv_len)  # kept alive: the struct holds their addresses
+        self.struct = CpPagedKv(_ptr(k_cache), _ptr(v_cache), k_cache.shape[0], _ptr(tables), tables.shape[1],
+                                _ptr(kv_len), self.n_seqs, self.n_heads)
+        self.ref = ctypes.byref(self.struct)
+
+    def check_rows(self, n_rows: int, q_start):
+        """q_start's checks; its address."""
+        import torch
+        if q_start is None:
+            return None
+        if q_start.dtype != torch.int32 or q_start.dim() != 1 or q_start.shape[0] != self.n_seqs + 1:
+            raise ValueError(f"q_start must be int32 [{self.n_seqs + 1}]")
+        _dev(q_start, "q_start")
+        return q_start.data_ptr()
+
+
+def attn_paged_workspace_size(kv: PagedKV, n_rows: int, max_q: int, n_heads_q: int) -> int:
+    """cp_attn_paged_workspace_size: bytes for up to n_rows rows, max_q of a sequence."""
+    n = lib.cp_attn_paged_workspace_size(kv.n_seqs, n_rows, max_q, n_heads_q, kv.n_heads)
+    if n == 0 and last_error():
+        raise CpError(CP_ERR_INVALID, last_error())
+    return n
+
+
+def _check_out(o, lse, rows: int, heads: int, D: int):
+    import torch
+    if o.dtype != torch.bfloat16 or not o.is_cuda or not o.is_contiguous() or o.dim() != 3 or o.shape[0] < rows \
+            or o.shape[1] != heads or o.shape[2] != D:
+        _dev(o, "o", torch.bfloat16, rows, (heads, D))
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.dim() != 2
+                            or lse.shape[0] < rows or lse.shape[1] != heads):
+        _dev(lse, "lse", torch.float32, rows, (heads,))
+
+
+def attn_paged(kv: PagedKV, q, o, workspace, lse=None, q_start=None, max_q: Optional[int] = None, window: int = 0,
+               n_sink: int = 0, softmax_scale: float = 0.0, stream=None):
+    """cp_attn_paged on the given (or current torch) stream: q bf16 [rows, Hq,
+    128] (rows may be strided), o bf16 and lse float32 of as many rows.  With
+    q_start (int32 [n_seqs + 1], on the GPU) max_q is the most rows of a
+    sequence; without, every sequence has rows / n_seqs.  ``workspace`` is a
+    uint8 GPU tensor of attn_paged_workspace_size bytes."""
+    rows, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    stride = _rows_of(q, "q", Hq, kv.head_dim)
+    start = kv.check_rows(rows, q_start)
+    if start is not None and max_q is None:
+        raise ValueError("max_q is needed with q_start")
+    _check_out(o, lse, rows, Hq, kv.head_dim)
+    _dev(workspace, "workspace")
+    _same_device(kv.device, (("q", q), ("o", o), ("lse", lse), ("q_start", q_start), ("workspace", workspace)), stream)
+    _check(lib.cp_attn_paged(kv.ref, q.data_ptr(), stride, rows, start, max_q or 0, Hq, kv.head_dim, softmax_scale,
+                             window, n_sink, o.data_ptr(), _ptr(lse), workspace.data_ptr(),
+                             workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+def attn_window_workspace_size(plan: CpRankPlan, n_heads_q: int, n_heads_kv: int) -> int:
+    """cp_attn_window_workspace_size."""
+    n = lib.cp_attn_window_workspace_size(ctypes.byref(plan), n_heads_q, n_heads_kv)
+    if n == 0 and last_error():
+        raise CpError(CP_ERR_INVALID, last_error())
+    return n
+
+
+def attn_window(plan: CpRankPlan, q, k_new, v_new, o, workspace, window: int, n_sink: int = 0, lse=None, k_cache=None,
+                v_cache=None, block_table=None, out_order: int = CP_OUT_LOCAL, softmax_scale: float = 0.0, stream=None):
+    """cp_attn_window on the given (or current torch) stream: the rank's rows q
+    bf16 [n_rows, Hq, 128] through a sliding window over the paged prefix
+    (caches [blocks, 16, Hkv, 128], needed when the plan has one) and k_new,
+    v_new bf16 [R, Hkv, 128].  o bf16 (and lse float32) has the rank's rows, or
+    R rows with out_order=CP_OUT_SEQUENCE."""
+    import torch
+    D = CP_HEAD_DIM
+    if q.dim() != 3 or k_new.dim() != 3:
+        raise ValueError("q and k_new must have shape [rows, heads, 128]")
+    Hq, Hkv = q.shape[1], k_new.shape[1]
+    _dev(q, "q", torch.bfloat16, plan.n_rows, (Hq, D))
+    _dev(k_new, "k_new", torch.bfloat16, plan.new_len, (Hkv, D))
+    _dev(v_new, "v_new", torch.bfloat16, plan.new_len, (Hkv, D))
+    if out_order not in (CP_OUT_LOCAL, CP_OUT_SEQUENCE):
+        raise ValueError("out_order must be CP_OUT_LOCAL or CP_OUT_SEQUENCE")
+    _check_out(o, lse, plan.new_len if out_order == CP_OUT_SEQUENCE else plan.n_rows, Hq, D)
+    n_blocks = table_len = 0
+    if plan.prefix_len > 0:
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache), ("block_table", block_table)):
+            if t is None:
+                raise ValueError(f"{name} is needed: the plan has a cached prefix")
+        _dev(k_cache, "k_cache", torch.bfloat16, None, (CP_KV_BLOCK_TOKENS, Hkv, D))
+        _dev(v_cache, "v_cache", torch.bfloat16, k_cache.shape[0], (CP_KV_BLOCK_TOKENS, Hkv, D))
+        _dev(block_table, "block_table", torch.int32)
+        n_blocks, table_len = k_cache.shape[0], block_table.numel()
+    else:
+        k_cache = v_cache = block_table = None
+    _dev(workspace, "workspace")
+    _same_device(q.device, (("k_new", k_new), ("v_new", v_new), ("o", o), ("lse", lse), ("k_cache", k_cache),
+                            ("v_cache", v_cache), ("block_table", block_table), ("workspace", workspace)), stream)
+    _check(lib.cp_attn_window(ctypes.byref(plan), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache),
+                              n_blocks, _ptr(block_table), table_len, Hq, Hkv, D, softmax_scale, window, n_sink,
+                              _ptr(o), _ptr(lse), out_order, _ptr(workspace),
+                              workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+# --- pages of a cache -------------------------------------------------------------------
+
+def kv_append(kv: PagedKV, k_rows, v_rows, q_start=None, stream=None):
+    """cp_kv_append: the batch's new rows k_rows, v_rows bf16 [rows, Hkv, D]
+    (rows may be strided) to the last positions of their sequences; q_start as
+    in attn_paged."""
+    k_stride = _rows_of(k_rows, "k_rows", kv.n_heads, kv.head_dim)
+    v_stride = _rows_of(v_rows, "v_rows", kv.n_heads, kv.head_dim)
+    rows = k_rows.shape[0]
+    if v_rows.shape[0] != rows:
+        raise ValueError("k_rows and v_rows differ in rows")
+    start = kv.check_rows(rows, q_start)
+    _same_device(kv.device, (("k_rows", k_rows), ("v_rows", v_rows), ("q_start", q_start)), stream)
+    _check(lib.cp_kv_append(kv.ref, k_rows.data_ptr(), v_rows.data_ptr(), k_stride, v_stride, rows, start, kv.head_dim,
+                            _stream_handle(stream)))
+
+
+class _Caches:
+    """Caches [blocks, ...] of equal shape and type as the pages calls take them."""
+
+    def __init__(self, caches):
+        n = len(caches)
+        if n > CP_KV_MAX_CACHES:
+            raise ValueError(f"at most {CP_KV_MAX_CACHES} caches")
+        for i, t in enumerate(caches):
+            _dev(t, f"caches[{i}]")
+            if t.dim() < 2 or t.shape != caches[0].shape or t.dtype != caches[0].dtype or t.device != caches[0].device:
+                raise ValueError("the caches must have one shape [blocks, ...], type and device")
+        self.tensors = tuple(caches)
+        self.n = n
+        self.n_blocks = caches[0].shape[0] if n else 0
+        self.page_bytes = math.prod(caches[0].shape[1:]) * caches[0].element_size() if n else 0
+        self.ptrs = (ctypes.c_void_p * max(1, n))(*[_ptr(t) for t in caches])
+
+
+class KVPool:
+    """Page tables int32 [n_seqs, pages], lengths int32 [n_seqs] and reference
+    counts int32 [blocks] of a pool's sequences (cp_kv_pool), and the caches
+    [blocks, ...] (K and V of every layer) whose pages they name.  Made once for
+    buffers that an engine keeps."""
+
+    def __init__(self, tables, kv_len, refs, caches=()):
+        import torch
+        _dev(tables, "tables", torch.int32)
+        if tables.dim() != 2:
+            raise ValueError("tables must have shape [n_seqs, pages]")
+        _dev(kv_len, "kv_len", torch.int32, tables.shape[0])
+        _dev(refs, "refs", torch.int32)
+        if kv_len.dim() != 1 or refs.dim() != 1:
+            raise ValueError("kv_len and refs must have one dimension")
+        self.caches = _Caches(tuple(caches))
+        if self.caches.n and self.caches.n_blocks != refs.shape[0]:
+            raise ValueError("the caches must hold as many pages as refs")
+        self.device = tables.device
+        for name, t in (("kv_len", kv_len), ("refs", refs), ("caches", self.caches.tensors[0] if caches else None)):
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{name} is on {t.device}, tables on {self.device}")
+        self.tensors = (tables, kv_len, refs)
+        self.struct = CpKvPool(_ptr(tables), tables.shape[1], _ptr(kv_len), _ptr(refs), refs.shape[0],
+                               tables.shape[0], 0)
+        self.ref = ctypes.byref(self.struct)
+
+    def check_lists(self, stream, missing=None, **lists) -> int:
+        """The lists' common length: int32 tensors of one dimension on the pool's device."""
+        import torch
+        n = None
+        for name, t in lists.items():
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+                _dev(t, name, torch.int32)
+                raise ValueError(f"{name} must have one dimension")
+            if n is not None and t.shape[0] != n:
+                raise ValueError("the lists differ in length")
+            n = t.shape[0]
+        if missing is not None:
+            _dev(missing, "missing", torch.int32, 1)
+            lists["missing"] = missing
+        _same_device(self.device, lists.items(), stream)
+        return n
+
+
+def kv_copy_pages(caches, src, dst, stream=None):
+    """cp_kv_copy_pages: page src[i] to page dst[i] (int32 GPU tensors) in every
+    one of ``caches`` (tensors [blocks, ...], or a KVPool's)."""
+    import torch
+    c = caches.caches if isinstance(caches, KVPool) else _Caches(tuple(caches))
+    if c.n == 0:
+        raise ValueError("at least one cache")
+    for name, t in (("src", src), ("dst", dst)):
+        _dev(t, name, torch.int32)
+    if src.dim() != 1 or dst.shape != src.shape:
+        raise ValueError("src and dst must have one dimension and one length")
+    _same_device(c.tensors[0].device, (("src", src), ("dst", dst)), stream)
+    _check(lib.cp_kv_copy_pages(c.ptrs, c.n, c.n_blocks, c.page_bytes, _ptr(src), _ptr(dst), src.shape[0],
+                                _stream_handle(stream)))
+
+
+def kv_reserve(pool: KVPool, seqs, add, missing, stream=None):
+    """cp_kv_reserve: room for add[i] more tokens of sequence seqs[i]; missing
+    int32 [1] receives how many entries got none."""
+    n = pool.check_lists(stream, missing, seqs=seqs, add=add)
+    _check(lib.cp_kv_reserve(pool.ref, _ptr(seqs), _ptr(add), n, _ptr(missing), _stream_handle(stream)))
+
+
+def kv_fork(pool: KVPool, parents, children, missing, stream=None):
+    """cp_kv_fork: sequence children[i] continues parents[i], sharing its full
+    pages; a page filled in part is copied in every cache of the pool."""
+    n = pool.check_lists(stream, missing, parents=parents, children=children)
+    c = pool.caches
+    _check(lib.cp_kv_fork(pool.ref, c.ptrs, c.n, c.page_bytes, _ptr(parents), _ptr(children), n, _ptr(missing),
+                          _stream_handle(stream)))
+
+
+def kv_free(pool: KVPool, seqs, begin, end, stream=None):
+    """cp_kv_free: the pages of sequence seqs[i] whose tokens lie in [begin[i], end[i])."""
+    n = pool.check_lists(stream, seqs=seqs, begin=begin, end=end)
+    _check(lib.cp_kv_free(pool.ref, _ptr(seqs), _ptr(begin), _ptr(end), n, _stream_handle(stream)))
+
+
+def kv_compact_workspace_size(pool: KVPool) -> int:
+    """cp_kv_compact_workspace_size of the pool."""
+    return lib.cp_kv_compact_workspace_size(pool.struct.n_blocks)
+
+
+def kv_compact(pool: KVPool, workspace, stream=None):
+    """cp_kv_compact: the pool's pages in use to its front, tables and counts with them."""
+    _dev(workspace, "workspace")
+    _same_device(pool.device, (("workspace", workspace),), stream)
+    c = pool.caches
+    _check(lib.cp_kv_compact(pool.ref, c.ptrs, c.n, c.page_bytes, _ptr(workspace),
+                             workspace.numel() * workspace.element_size(), _stream_handle(stream)))

@@ -1,0 +1,458 @@
+// Attention over a paged cache of blocks of few rows: the step that decodes one
+// token (or a few) of every sequence.  A row is a (position, query head) pair of
+// one KV head, so that grouped query heads share every key that is read.
+//
+// For the row at position p, over the visible keys j (j <= p, within the window
+// or among the first tokens):  x_j = scale q.k_j,  LSE = ln sum_j e^{x_j},
+// O = sum_j e^{x_j - LSE} v_j, in one pass with a running maximum and sum (Milakov
+// & Gimelshein 2018; Dao 2023).  Scores, statistics and O are fp32; the weights
+// are rounded to bf16 for the second product (at most half a step, 2^-9 of each)
+// and O is divided by the sum of the rounded ones; O is rounded once more as it is
+// stored.
+//
+// Bound by HBM: 512 bytes per key and KV head, each read once, for 16 to 64 rows.
+// The walks of all blocks, in steps of 128 keys, are cut into kShares equal parts,
+// one per workgroup and compute unit, wherever the cut falls (the lengths are
+// read from the device, so that a captured launch follows them): no unit waits
+// for another's longer sequence.  A part that ends inside a walk leaves a partial
+// result, and rows_merge_kernel combines a walk's.  Each of a workgroup's four
+// waves takes every fourth tile of 32 keys into its own LDS (two tiles of K and of
+// V, loaded directly, the next ones in flight while one is used), so the waves
+// meet only at the end of a walk.
+#include <hip/hip_runtime.h>
+
+#include "attn_tile.h"
+
+namespace cpattn {
+
+namespace {
+
+using namespace tile;
+
+constexpr int kWaves = kRowsThreads / 64;
+constexpr int kWaveBytes = 4 * kTileBytes;  // two K tiles, two V tiles
+constexpr int kLoads = kTileBytes / 1024;   // direct-to-LDS loads of a tile and tensor, 1 KB each
+
+__device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
+  return (int)(((int64_t)n * p.G + p.block_rows - 1) / p.block_rows);
+}
+
+__device__ __forceinline__ Walk block_walk(const PagedParams& p, const Segment& s, int block) {
+  const int r0 = block * p.block_rows;
+  const int rows = s.n * p.G;
+  return walk_of(p, s, r0, r0 + p.block_rows < rows ? r0 + p.block_rows : rows);
+}
+
+// Steps of a walk; one at least, which stores the rows of a block without keys.
+__device__ __forceinline__ int steps_of(const Walk& w) {
+  const int n = (w.n + kWaves - 1) / kWaves;
+  return n > 0 ? n : 1;
+}
+
+__device__ __forceinline__ int64_t segment_steps(const PagedParams& p, int s) {
+  const Segment x = segment_at(p, s);
+  int64_t n = 0;
+  for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) n += steps_of(block_walk(p, x, b));
+  return n;
+}
+
+// The start of this workgroup's share and its length in steps.  Every thread
+// counts the steps of its run of segments, and a scan finds the one that the
+// share begins in.  The heads of a block follow one another: neighbouring
+// workgroups read the same pages.
+struct Share {
+  ShareStart at;
+  int64_t n;
+};
+
+__device__ Share find_share(const PagedParams& p, int share) {
+  __shared__ int64_t wave_sum[kWaves];
+  __shared__ Share found;
+  const int tid = threadIdx.x;
+  const int per = (p.n_segments + kRowsThreads - 1) / kRowsThreads;
+  const int s0 = tid * per < p.n_segments ? tid * per : p.n_segments;
+  const int s1 = s0 + per < p.n_segments ? s0 + per : p.n_segments;
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) mine += segment_steps(p, s);
+  int64_t before = mine;
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    const int64_t x = __shfl_up(before, k);
+    if ((tid & 63) >= k) before += x;
+  }
+  if ((tid & 63) == 63) wave_sum[tid >> 6] = before;
+  if (tid == 0) found = Share{{0, 0, 0, 0}, 0};
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < (tid >> 6)) before += wave_sum[w];
+    total += wave_sum[w];
+  }
+  before -= mine;
+  total *= p.Hkv;
+  // No share between two others is empty: with fewer steps the last ones are.
+  const int64_t n = total < p.n_shares ? total : p.n_shares;
+  const int64_t u0 = share < n ? total * share / n : total, u1 = share < n ? total * (share + 1) / n : total;
+  if (u1 > u0 && u0 >= before * p.Hkv && u0 < (before + mine) * p.Hkv) {
+    int64_t u = u0 - before * p.Hkv;
+    for (int s = s0; s < s1; ++s) {
+      const Segment x = segment_at(p, s);
+      for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) {
+        const int n = steps_of(block_walk(p, x, b));
+        if (u < (int64_t)n * p.Hkv) {
+          if (u >= 0) found = Share{{s, b, (int)(u / n), (int)(u % n)}, u1 - u0};
+          u = -1;
+          s = s1;
+          break;
+        }
+        u -= (int64_t)n * p.Hkv;
+      }
+    }
+  }
+  __syncthreads();
+  return found;
+}
+
+// One tile's loads of K (tensor 0) or V: 1 KB each, four keys of 256 bytes.  `off`
+// are this lane's offsets within a half (four loads of it).
+__device__ __forceinline__ void load_tile(const PagedParams& p, const Walk& w, int t0, int kvh, int pages, int first,
+                                          const uint32_t (&off)[4], int lane, uint32_t dst, int tensor) {
+  const unsigned char* cache = tensor ? p.v_cache : p.k_cache;
+  const unsigned char* fresh = tensor ? p.v_new : p.k_new;
+  const bool whole = whole_tile(w, t0);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int hp = t0 + half * kBlockTokens;
+    const HalfSource h = half_source(p, __builtin_amdgcn_readlane(pages, first + half), hp, kvh);
+    const unsigned char* base = (h.paged ? cache : fresh) + h.offset;
+    const bool plain = whole && !h.none;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const unsigned char* from = base + off[q];
+      if (!plain && (h.none || !walked(w, hp + 4 * q + (lane >> 4)))) from = g_zeros + ((lane & 15) << 4);
+      load_lds_from(from, dst + half * kHalfBytes + q * 1024);
+    }
+  }
+}
+
+template <int NB>
+__global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * kWaveBytes];
+  __shared__ float stat[3][kWaves][16 * NB];  // per wave and row: maximum, sum, sum of the rounded weights
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, i16 = lane & 15;
+  const Share share = find_share(p, blockIdx.x);
+  if (tid == 0) p.starts[blockIdx.x] = share.n ? share.at : ShareStart{-1, 0, 0, 0};
+  if (share.n == 0) return;
+
+  unsigned char* const mine = smem + wave * kWaveBytes;
+  const uint32_t lds = lds_addr(mine);
+  uint32_t off[4];  // this lane's key and chunk in each load of a half
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int key = 4 * q + g;
+    off[q] = (uint32_t)(key * p.kv_stride) + ((i16 ^ swizzle(key)) << 4);
+  }
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
+
+  int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
+  int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
+  int64_t left = share.n;
+  Segment s = segment_at(p, seg);
+  for (;;) {
+    const Walk w = block_walk(p, s, block);
+    const int n_steps = steps_of(w);
+    const int stop = left < n_steps - step ? step + (int)left : n_steps;
+    const int rows = s.n * p.G, r0 = block * p.block_rows;
+
+    // Rows past the block's end repeat its last one and are not stored.
+    int pos[NB];
+    bf16x8 qf[NB][4];  // B of S^T = K Q^T: row i16 of block b, head dims 32 step + 8 g ..
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      int r = r0 + 16 * b + i16;
+      r = r < rows ? r : rows - 1;
+      const int at = (int)((unsigned)r / (unsigned)p.G), h = r - at * p.G;
+      pos[b] = s.pos0 + at;
+      const uint16_t* q = p.q + (s.q_row + at) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
+    }
+    f32x4 o[8][NB], psum[NB];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
+      psum[b] = f32x4{};
+      m[b] = kNoMax;
+      l[b] = 0.f;
+    }
+
+    // This wave's tiles: kWaves * j + wave for j in [step, stop), below w.n.
+    const int t_end = w.n < kWaves * stop ? w.n : kWaves * stop;
+    const int n_mine = (t_end - kWaves * step - wave + kWaves - 1) / kWaves;
+    int ids = -1;  // pages of the halves of tiles 32 (j / 32) .. of this wave, one per lane
+    auto tile_at = [&](int j) { return tile_begin(w, kWaves * (step + j) + wave); };
+    auto fetch_ids = [&](int j) {
+      ids = -1;
+      const int jj = j + (lane >> 1);
+      if (jj < n_mine) ids = page_of(p, s, tile_at(jj) + (lane & 1) * kBlockTokens);
+    };
+    auto load = [&](int j, int buf, int tensor) {
+      load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + (2 * tensor + buf) * kTileBytes, tensor);
+    };
+    // Tiles past the last load it again, into buffers that nobody reads: every
+    // iteration has the same number of loads in flight.
+    int ids_of = 0;
+    if (n_mine > 0) {
+      fetch_ids(0);
+#pragma unroll 1
+      for (int x = 0; x < 4; ++x) load((x >> 1) < n_mine ? (x >> 1) : n_mine - 1, x >> 1, x & 1);
+    }
+    for (int j = 0; j < n_mine; ++j) {
+      const int t0 = tile_at(j);
+      const unsigned char* kt = mine + (j & 1) * kTileBytes;
+      const unsigned char* vt = kt + 2 * kTileBytes;
+      const int jn = j + 2 < n_mine ? j + 2 : n_mine - 1;
+      if ((jn & ~31) != ids_of) {
+        ids_of = jn & ~31;
+        fetch_ids(ids_of);
+      }
+      __builtin_amdgcn_s_waitcnt(wait_vm(3 * kLoads));  // K of tile j is in LDS
+      asm volatile("" ::: "memory");
+      f32x4 sc[NB][2];
+      {
+        bf16x8 kf[2][4];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) kf[half][d] = k_frag(kt, lane, half, d);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            sc[b][half] = f32x4{};
+#pragma unroll
+            for (int d = 0; d < 4; ++d) sc[b][half] = mfma16(kf[half][d], qf[b][d], sc[b][half]);
+          }
+      }
+      // The K fragments are in registers (the products used them): the buffer is free.
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      asm volatile("" ::: "memory");
+      load(jn, j & 1, 0);
+
+      const bool open = open_tile(p, w, t0);
+      bf16x8 pf[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (!open) mask_scores(p, sc[b], t0, g, pos[b]);
+        float top = sc[b][0][0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) top = __builtin_elementwise_maximum(top, sc[b][r >> 2][r & 3]);
+        const float m_new = __builtin_elementwise_maximum(m[b], quad_max(top) * p.scale_log2);
+        const float alpha = __builtin_amdgcn_exp2f(m[b] - m_new);
+        m[b] = m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][r >> 2][r & 3], p.scale_log2, -m_new));
+          sum += x;
+          pf[b][r] = (__bf16)x;
+        }
+        l[b] = l[b] * alpha + sum;
+        psum[b] *= alpha;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
+      __builtin_amdgcn_s_waitcnt(wait_vm(3 * kLoads));  // V of tile j
+      asm volatile("" ::: "memory");
+      // Keys hidden from every row are zeros; hidden from some, they may be anything.
+      if (__builtin_expect(!open && w.p_lo != w.p_hi && not_finite(vt, lane), 0)) {
+        pv_not_finite<NB>(vt, lane, pf, o);
+      } else {
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+          const bf16x8 vf = v_frag(vt, lane, db);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) o[db][b] = mfma16(vf, pf[b], o[db][b]);
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      asm volatile("" ::: "memory");
+      load(jn, j & 1, 1);
+    }
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no load may still be writing LDS
+    asm volatile("" ::: "memory");
+
+    // The four waves' results, unnormalised, row by row through LDS: float4 c of row
+    // r at slot c ^ (r % 16) of its row.
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int r = 16 * b + i16;
+      const float sum = quad_sum(l[b]);
+      if (g == 0) {
+        stat[0][wave][r] = m[b];
+        stat[1][wave][r] = sum;
+        stat[2][wave][r] = psum[b][0];
+      }
+#pragma unroll
+      for (int db = 0; db < 8; ++db)
+        *reinterpret_cast<f32x4*>(mine + r * (kHeadDim * 4) + (((4 * db + g) ^ i16) << 4)) = o[db][b];
+    }
+    __syncthreads();
+    const bool part = step > 0 || stop < n_steps;
+    float* slot = p.slots + (2 * (size_t)blockIdx.x + (step > 0 ? 0 : 1)) * slot_floats(16 * NB);
+    for (int x = tid; x < 16 * NB * 16; x += kRowsThreads) {  // 8 values of a row each
+      const int r = x >> 4, c = (x & 15) * 2;
+      float top = kNoMax;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
+      float sum = 0.f, rounded = 0.f;
+      f32x4 a0 = {}, a1 = {};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float wk = __builtin_amdgcn_exp2f(stat[0][k][r] - top);
+        sum += wk * stat[1][k][r];
+        rounded += wk * stat[2][k][r];
+        const unsigned char* row = smem + k * kWaveBytes + r * (kHeadDim * 4);
+        a0 += wk * *reinterpret_cast<const f32x4*>(row + ((c ^ (r & 15)) << 4));
+        a1 += wk * *reinterpret_cast<const f32x4*>(row + (((c + 1) ^ (r & 15)) << 4));
+      }
+      const bool live = top > 0.5f * kNoMax && sum > 0.f;  // false for a NaN too
+      const float inv = live ? 1.f / rounded : (sum != sum ? sum : 0.f);
+      const float lse = live ? top * kLn2 + logf(sum) : -INFINITY;
+      a0 *= inv;
+      a1 *= inv;
+      if (part) {
+        // A NaN among the scores is an LSE of NaN here: the merge tells it from a part without keys.
+        *reinterpret_cast<f32x4*>(slot + r * kHeadDim + 4 * c) = a0;
+        *reinterpret_cast<f32x4*>(slot + r * kHeadDim + 4 * c + 4) = a1;
+        if (c == 0) slot[16 * NB * kHeadDim + r] = sum != sum ? sum : lse;
+      } else if (r0 + r < rows) {
+        const int at = (int)((unsigned)(r0 + r) / (unsigned)p.G);
+        const int64_t out = (s.o_row + at) * p.Hq + kvh * p.G + (r0 + r - at * p.G);
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = (__bf16)a0[e];
+          v[4 + e] = (__bf16)a1[e];
+        }
+        *reinterpret_cast<bf16x8*>(p.o + out * kHeadDim + 4 * c) = v;
+        if (c == 0 && p.lse) p.lse[out] = lse;
+      }
+    }
+    left -= stop - step;
+    if (left <= 0) return;
+    __syncthreads();  // the LDS is free for the next walk's tiles
+    step = 0;
+    if (++kvh == p.Hkv) {
+      kvh = 0;
+      ++block;
+      while (block >= blocks_of(p, s.n)) {
+        block = 0;
+        if (++seg >= p.n_segments) return;  // (never: a share ends with the last walk)
+        s = segment_at(p, seg);
+      }
+    }
+  }
+}
+
+// The parts of a walk that was cut, combined (they cover disjoint keys): LSE = M +
+// ln sum_k e^{LSE_k - M}, O = sum_k e^{LSE_k - LSE} O_k.  A walk's first part is
+// the second slot of the share that it begins in, the others are the first slots of
+// the shares that begin within it.  Block (x, y): the walk that share x begins
+// within, if it is the first to do so, rows 4 y .. 4 y + 3, one wave each.
+__global__ __launch_bounds__(256) void rows_merge_kernel(PagedParams p) {
+  const int share = blockIdx.x + 1;
+  const ShareStart at = p.starts[share];
+  if (at.segment < 0 || at.step == 0) return;
+  auto same = [&](const ShareStart& x) { return x.segment == at.segment && x.block == at.block && x.kvh == at.kvh; };
+  if (share > 1) {
+    const ShareStart before = p.starts[share - 1];
+    if (same(before) && before.step > 0) return;
+  }
+  const Segment s = segment_at(p, at.segment);
+  const int lane = threadIdx.x & 63;
+  const int r = 4 * blockIdx.y + (threadIdx.x >> 6);
+  const int row = at.block * p.block_rows + r;
+  if (r >= p.block_rows || row >= s.n * p.G) return;
+  const size_t size = slot_floats(p.block_rows);
+  // The walk's shares: this one and those after it that begin within the walk.
+  int n = 1;
+  for (;; n += 64) {
+    const int k = share + n + lane;
+    bool in = k < p.n_shares;
+    if (in) {
+      const ShareStart x = p.starts[k];
+      in = same(x) && x.step > 0;
+    }
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
+    if (mask != ~0ull) {
+      n += __builtin_ctzll(~mask);
+      break;
+    }
+  }
+  // Part 0 lies in the share before; part k in share + k - 1.
+  auto slot_of = [&](int k) { return p.slots + (2 * (size_t)(share - 1 + k) + (k == 0 ? 1 : 0)) * size; };
+  auto lse_of = [&](int k) { return slot_of(k)[(size_t)p.block_rows * kHeadDim + r]; };
+  float top = -INFINITY;
+  for (int k = lane; k <= n; k += 64) top = __builtin_elementwise_maximum(top, lse_of(k));
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) top = __builtin_elementwise_maximum(top, __shfl_xor(top, k));
+  float2 acc = make_float2(0.f, 0.f);
+  float sum = 0.f;
+  if (top != -INFINITY) {
+    for (int k0 = 0; k0 <= n; k0 += 64) {
+      const float l = k0 + lane <= n ? lse_of(k0 + lane) : -INFINITY;
+      const float w = l == -INFINITY ? 0.f : expf(l - top);
+      sum += w;
+      const int end = n + 1 - k0 < 64 ? n + 1 - k0 : 64;
+      for (int k = 0; k < end; ++k) {
+        const float wk = __shfl(w, k);
+        const float2 v = reinterpret_cast<const float2*>(slot_of(k0 + k) + (size_t)r * kHeadDim)[lane];
+        acc.x += wk * v.x;
+        acc.y += wk * v.y;
+      }
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+    acc.x /= sum;
+    acc.y /= sum;
+  }
+  const int i = (int)((unsigned)row / (unsigned)p.G);
+  const int64_t out = (s.o_row + i) * p.Hq + at.kvh * p.G + (row - i * p.G);
+  const bf16x2 v = {(__bf16)acc.x, (__bf16)acc.y};
+  reinterpret_cast<bf16x2*>(p.o + out * kHeadDim)[lane] = v;
+  if (lane == 0 && p.lse) p.lse[out] = top == top && top != -INFINITY ? top + logf(sum) : -INFINITY;
+}
+
+int launched(const char* who) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CP_OK : fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));
+}
+
+}  // namespace
+
+int launch_attn_rows(const PagedParams& p, void* stream, const char* who) {
+  const dim3 grid((unsigned)p.n_shares), block(kRowsThreads);
+  hipStream_t st = (hipStream_t)stream;
+  if (p.block_rows == 16)
+    hipLaunchKernelGGL(attn_rows_kernel<1>, grid, block, 0, st, p);
+  else if (p.block_rows == 32)
+    hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL(attn_rows_kernel<4>, grid, block, 0, st, p);
+  int rc = launched(who);
+  if (rc != CP_OK || p.n_shares == 1) return rc;
+  hipLaunchKernelGGL(rows_merge_kernel, dim3((unsigned)p.n_shares - 1, (unsigned)(p.block_rows / 4)), dim3(256), 0, st, p);
+  return launched(who);
+}
+
+}  // namespace cpattn

@@ -1,0 +1,276 @@
+// Building blocks of the attention kernels over a paged cache (attn_paged.hip,
+// attn_chunk.hip): where a segment's keys lie, which of them a block of rows
+// walks, and 32-key tiles of K and V in LDS as operands of the matrix cores.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "paged.h"
+
+namespace cpattn {
+namespace tile {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTileKeys = 32;
+constexpr int kRowBytes = kHeadDim * 2;
+constexpr int kHalfBytes = kBlockTokens * kRowBytes;  // one page's keys of one head
+constexpr int kTileBytes = kTileKeys * kRowBytes;
+
+// Exponents are kept in units of log2.  A running maximum starts at a finite
+// value far below any score's: a masked score (-inf) then weighs
+// exp2(-inf - kNoMax) = 0 without a special case.
+constexpr float kNoMax = -1e30f;
+constexpr float kLn2 = 0.69314718055994531f;
+
+// ---------------------------------------------------------------------------
+// Segments: consecutive query positions that share their keys -- one sequence
+// of a batch, or one chunk of a rank.
+
+struct Segment {
+  int64_t q_row;         // its first row in q
+  int64_t o_row;         // and in o and lse
+  int n;                 // query positions
+  int pos0;              // position of the first (negative: it sees no key)
+  const int32_t* table;  // pages of its positions
+};
+
+// Positions are below 2^30: lengths beyond (or below 0) are contents that the
+// host cannot check, and are cut to it.
+__device__ __forceinline__ Segment segment_at(const PagedParams& p, int s) {
+  Segment x;
+  if (p.n_chunks) {
+    x.q_row = s ? p.chunk_row[1] : p.chunk_row[0];
+    x.o_row = s ? p.chunk_out[1] : p.chunk_out[0];
+    x.n = s ? p.chunk_len[1] : p.chunk_len[0];
+    x.pos0 = s ? p.chunk_pos[1] : p.chunk_pos[0];
+    x.table = p.tables;
+    return x;
+  }
+  const int n_rows = (int)p.n_rows;
+  int a = s * p.uniform_q, b = a + p.uniform_q;
+  if (p.q_start) {
+    a = p.q_start[s];
+    b = p.q_start[s + 1];
+  }
+  a = a < 0 ? 0 : (a > n_rows ? n_rows : a);
+  b = b < a ? a : (b > n_rows ? n_rows : b);
+  int len = p.kv_len[s];
+  len = len < 0 ? 0 : (len > kMaxTokens ? kMaxTokens : len);
+  x.q_row = x.o_row = a;
+  x.n = b - a < p.max_q ? b - a : p.max_q;
+  x.pos0 = len - (b - a);
+  x.table = p.tables + (int64_t)s * p.table_stride;
+  return x;
+}
+
+// Row r of a segment's KV head is query head r % G of position r / G.
+// The keys that rows [r0, r1) walk, in tiles of 32: the first tokens that stay
+// visible, then the window of the first row up to the last row's position (from
+// a page's first key).  Without a window, or where the two meet, all from 0.
+struct Walk {
+  int end;         // one past the last key that a row sees
+  int lo;          // first key of the window of the first row (0: none)
+  int sink;        // keys below it are visible to every row behind them
+  int p_lo, p_hi;  // positions of the first and the last row
+  int n_sink_tiles;
+  int base;        // first key of the tiles after the sink tiles
+  int n;           // tiles
+};
+
+__device__ __forceinline__ Walk walk_of(const PagedParams& p, const Segment& s, int r0, int r1) {
+  Walk w;
+  w.p_lo = s.pos0 + (int)((unsigned)r0 / (unsigned)p.G);
+  w.p_hi = s.pos0 + (int)((unsigned)(r1 - 1) / (unsigned)p.G);
+  w.end = w.p_hi + 1 > 0 ? w.p_hi + 1 : 0;
+  w.lo = 0;
+  w.sink = 0;
+  w.n_sink_tiles = 0;
+  w.base = 0;
+  if (p.window && w.p_lo - p.window + 1 > 0) {
+    w.lo = w.p_lo - p.window + 1;
+    w.sink = p.n_sink < w.end ? p.n_sink : w.end;
+    w.n_sink_tiles = (w.sink + kTileKeys - 1) / kTileKeys;
+    w.base = w.lo & ~(kBlockTokens - 1);
+    if (w.n_sink_tiles && w.base <= w.n_sink_tiles * kTileKeys) w.n_sink_tiles = w.base = 0;
+  }
+  w.n = w.n_sink_tiles + (w.end - w.base + kTileKeys - 1) / kTileKeys;
+  return w;
+}
+
+__device__ __forceinline__ int tile_begin(const Walk& w, int t) {
+  return t < w.n_sink_tiles ? t * kTileKeys : w.base + (t - w.n_sink_tiles) * kTileKeys;
+}
+
+// Some row of the block sees key j (no row sees the others: they read as zeros,
+// whatever the cache holds there).
+__device__ __forceinline__ bool walked(const Walk& w, int j) { return j < w.end && (j >= w.lo || j < w.sink); }
+
+// Every key of the tile at t0 is walked; and every row sees all of them.
+__device__ __forceinline__ bool whole_tile(const Walk& w, int t0) {
+  return t0 + kTileKeys <= w.end && (t0 >= w.lo || t0 + kTileKeys <= w.sink);
+}
+__device__ __forceinline__ bool open_tile(const PagedParams& p, const Walk& w, int t0) {
+  return t0 + kTileKeys <= w.p_lo + 1 &&
+         (!p.window || t0 > w.p_hi - p.window || t0 + kTileKeys <= p.n_sink);
+}
+
+// ---------------------------------------------------------------------------
+// K and V tiles in LDS.  A half is one page's 16 keys of one KV head, 256 bytes
+// each; 16-byte chunk c of key k (of the half) lies at slot c ^ swizzle(k) of the
+// key's 256 bytes.  The K reads (16 keys, one chunk) then touch every bank once,
+// and so do the transposed V reads (8 keys, two chunks).
+__device__ __forceinline__ int swizzle(int k) { return ((k & 7) << 1) | ((k >> 3) & 1); }
+
+__device__ __forceinline__ uint32_t lds_addr(const unsigned char* p) {
+  return (uint32_t)(uintptr_t)((const __attribute__((address_space(3))) unsigned char*)p);
+}
+
+// 256 zero bytes: what a key without a page, or that no row sees, reads.
+__device__ __attribute__((aligned(256))) unsigned char g_zeros[kRowBytes];
+
+// One direct-to-LDS load: lane l's 16 bytes at its address land at LDS byte lds_base
+// + 16 l.  Inline assembly, so that the compiler does not make every later LDS
+// read wait for it: the kernels count these loads themselves.  The LDS address is
+// an input bound to m0; one wait state between its write and the load.
+__device__ __forceinline__ void load_lds_from(const void* addr, uint32_t lds_base) {
+  asm volatile(
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, off\n\t" ::"v"(addr),
+      "{m0}"(__builtin_amdgcn_readfirstlane((int)lds_base))
+      : "memory");
+}
+
+// s_waitcnt immediate: at most n of this wave's vector-memory operations
+// outstanding (vmcnt[3:0] at [3:0], vmcnt[5:4] at [15:14]).
+constexpr int wait_vm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+// Where a half's keys lie: their page, or rows of k_new (same offsets for V).
+struct HalfSource {
+  int64_t offset;  // bytes from the cache's (or k_new's) start to key 0, this KV head
+  bool paged, none;
+};
+
+__device__ __forceinline__ HalfSource half_source(const PagedParams& p, int page, int hp, int kvh) {
+  HalfSource h;
+  h.paged = hp < p.paged_end;
+  h.none = h.paged && (uint32_t)page >= (uint32_t)p.n_blocks;
+  const int64_t key = h.paged ? (int64_t)page * kBlockTokens : (int64_t)(hp - p.paged_end);
+  h.offset = key * p.kv_stride + (int64_t)kvh * kRowBytes;
+  return h;
+}
+
+// The page of the half at position hp (any value where there is none to read).
+__device__ __forceinline__ int page_of(const PagedParams& p, const Segment& s, int hp) {
+  const int b = hp / kBlockTokens;
+  return hp < p.paged_end && b < p.table_len ? s.table[b] : -1;
+}
+
+// ---------------------------------------------------------------------------
+// Fragments (v_mfma_f32_16x16x32_bf16; lane 16 g + i).
+
+__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// A of S^T = K Q^T: key i of the half, head dims 32 step + 8 g ..
+__device__ __forceinline__ bf16x8 k_frag(const unsigned char* k, int lane, int half, int step) {
+  const int g = lane >> 4, i = lane & 15;
+  return *reinterpret_cast<const bf16x8*>(k + half * kHalfBytes + i * kRowBytes + (((4 * step + g) ^ swizzle(i)) << 4));
+}
+
+// A of O^T += V^T P^T: head dim 16 db + i, keys 4 g .. 4 g + 3 of each half, by
+// the transposing read.
+__device__ __forceinline__ bf16x8 v_frag(const unsigned char* v, int lane, int db) {
+  const int g = lane >> 4, i = lane & 15;
+  const int k = 4 * g + (i >> 2);
+  const unsigned char* at = v + k * kRowBytes + (((2 * db + ((i & 3) >> 1)) ^ swizzle(k)) << 4) + 8 * (i & 1);
+  typedef __attribute__((address_space(3))) s16x4* Lds;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + kHalfBytes));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Maximum (NaN if any is) and sum over the four lanes that hold one query.
+__device__ __forceinline__ float quad_max(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  x = __builtin_elementwise_maximum(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return __builtin_elementwise_maximum(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  x = __builtin_bit_cast(float, (unsigned)a[0]) + __builtin_bit_cast(float, (unsigned)a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return __builtin_bit_cast(float, (unsigned)b[0]) + __builtin_bit_cast(float, (unsigned)b[1]);
+}
+
+// Scores of keys that the row at position pos does not see become -inf.
+// s[half][r] is key t0 + 16 half + 4 g + r.
+__device__ __forceinline__ void mask_scores(const PagedParams& p, f32x4 (&s)[2], int t0, int g, int pos) {
+  const int first = t0 + 4 * g;
+  const int lo = p.window ? pos - p.window : -1;  // keys above it are in the window
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int j = first + 16 * half + r;
+      if (j > pos || (j <= lo && j >= p.n_sink)) s[half][r] = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);  // one comparison's masks at a time in scalar registers
+    }
+}
+
+// Whether the V tile holds an infinity or a NaN: its product with zeros is not 0.
+__device__ __forceinline__ bool not_finite(const unsigned char* v, int lane) {
+  f32x4 z = {};
+  bf16x8 zeros = {};
+#pragma unroll
+  for (int db = 0; db < 8; ++db) z = mfma16(v_frag(v, lane, db), zeros, z);
+  const bool bad = !(z[0] == 0.f && z[1] == 0.f && z[2] == 0.f && z[3] == 0.f);
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+
+// O^T += V^T P^T of such a tile, where some of its keys are hidden from some rows
+// of the block: a weight of 0 times an infinity would be a NaN.  The finite values
+// are added as ever; a row takes the others from the keys that it sees.
+template <int NB>
+__device__ __forceinline__ void pv_not_finite(const unsigned char* v, int lane, const bf16x8 (&pf)[NB],
+                                              f32x4 (&o)[8][NB]) {
+#pragma unroll
+  for (int db = 0; db < 8; ++db) {
+    const bf16x8 f = v_frag(v, lane, db);
+    bf16x8 fine, up, down, nan;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = (float)f[e];
+      fine[e] = (__bf16)(__builtin_isfinite(x) ? x : 0.f);
+      up[e] = (__bf16)(x == INFINITY ? 1.f : 0.f);
+      down[e] = (__bf16)(x == -INFINITY ? 1.f : 0.f);
+      nan[e] = (__bf16)(x != x ? 1.f : 0.f);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      bf16x8 seen;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) seen[e] = (__bf16)((float)pf[b][e] == 0.f ? 0.f : 1.f);
+      o[db][b] = mfma16(fine, pf[b], o[db][b]);
+      const f32x4 a = mfma16(up, seen, f32x4{}), c = mfma16(down, seen, f32x4{}), n = mfma16(nan, seen, f32x4{});
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (a[r] > 0.f) o[db][b][r] += INFINITY;
+        if (c[r] > 0.f) o[db][b][r] -= INFINITY;
+        if (n[r] > 0.f) o[db][b][r] = NAN;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+}  // namespace tile
+}  // namespace cpattn

@@ -1,0 +1,260 @@
+"""GPU checks of cp_attn_paged (single tokens, chunks, mixed batches; windows) and
+cp_kv_append against the float64 oracle."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import window as owin
+from paper_2609_04774_amd import cpattn as cp
+
+from paged_cases import B, D, DEV, Batch, compare, f64, randn
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(8, 2), (4, 4), (8, 1), (28, 4), (64, 8)]
+
+
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
+@pytest.mark.parametrize("new", [1, 2, 5])
+def test_decode_lengths(Hq, Hkv, new):
+    """Lengths around tile, page and step borders, none and one among them."""
+    lens = [0, 1, 5, 15, 16, 17, 31, 32, 33, 127, 128, 129, 300, 1111]
+    b = Batch(lens, [new] * len(lens), Hq, Hkv, seed=10 + new, uniform=True)
+    b.check(*b.run())
+
+
+@pytest.mark.parametrize("window,n_sink", [(1, 0), (1, 1), (16, 0), (33, 4), (100, 16), (100, 40), (127, 33), (5000, 7)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_decode_window(window, n_sink, new):
+    lens = [0, 1, 16, 33, 100, 133, 161, 500, 777]
+    b = Batch(lens, [new] * len(lens), 8, 2, seed=30 + window, uniform=True)
+    b.hide(window, n_sink)
+    b.check(*b.run(window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
+def test_ragged_chunks(Hq, Hkv):
+    """Chunks behind contexts of any length, sequences without rows, one token
+    and long chunks in one launch."""
+    new = [7, 0, 1, 130, 33, 64, 300, 1]
+    lens = [7, 90, 1, 131, 77, 400, 300, 640]
+    b = Batch(lens, new, Hq, Hkv, seed=50)
+    b.check(*b.run(), rows=np.array([0, 1, 15, 16, 31, 32, 63, 64, 129, 255, 256, 10**6]))
+
+
+@pytest.mark.parametrize("window,n_sink", [(1, 0), (20, 3), (64, 0), (200, 40), (1000, 5)])
+def test_chunk_window(window, n_sink):
+    new, lens = [257, 3, 90, 40], [600, 700, 90, 300]
+    b = Batch(lens, new, 8, 2, seed=60)
+    b.hide(window, n_sink)
+    b.check(*b.run(window, n_sink), window, n_sink, rows=np.arange(0, 300, 13))
+
+
+def test_one_long_sequence():
+    """Many shares of one walk, and their merge."""
+    b = Batch([20011], [1], 8, 2, seed=70, uniform=True)
+    b.check(*b.run())
+
+
+def test_more_sequences_than_threads():
+    rng = np.random.RandomState(5)
+    lens = rng.randint(0, 60, 700).tolist()
+    new = [min(int(x), t) for x, t in zip(rng.randint(0, 4, 700), lens)]
+    b = Batch(lens, new, 4, 2, seed=71)
+    b.check(*b.run())
+
+
+def test_rows_before_the_first_position():
+    """More new rows than positions: those below position 0 see no key."""
+    b = Batch([3, 0, 20], [5, 5, 5], 8, 2, seed=72, uniform=True)
+    o, lse = b.run()
+    assert (o[:2] == 0).all() and torch.isneginf(lse[:2]).all()
+    assert (o[5:10] == 0).all() and torch.isneginf(lse[5:10]).all()
+    b.check(o, lse)
+
+
+def test_rows_outside_the_sequences_are_left():
+    b = Batch([40, 50], [3, 4], 8, 2, seed=73)
+    b.q = torch.cat([b.q, b.q[:4]])
+    o, lse = b.run()
+    assert torch.isnan(o[7:]).all() and torch.isnan(lse[7:]).all()
+    b.check(o[:7], lse[:7])
+    b.q = b.q[:7]
+    b.max_q = 2  # rows past it are left too
+    o, _ = b.run()
+    assert not torch.isnan(o[[0, 1, 3, 4]]).any() and torch.isnan(o[[2, 5, 6]]).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new", [4, 100])
+def test_values_that_a_row_does_not_see(bad, new):
+    """A later token's K and V, infinite or NaN, change nothing for the rows before
+    it; the rows that see them show them."""
+    b = Batch([200], [new], 8, 2, seed=74)
+    at = 200 - new // 2
+    page, slot = int(b.tables[0, at // B]), at % B
+    b.vc[page, slot, 1, 5] = bad
+    b.v[0][at, 1, 5] = bad
+    o, lse = b.run()
+    want = f64(o)
+    early = new - new // 2
+    assert np.isfinite(want[:early]).all()
+    seen = want[early:, 4:, 5]
+    assert np.isnan(seen).all() if np.isnan(bad) else (seen == bad).all()
+    assert np.isfinite(np.delete(want[early:], 5, axis=2)).all() and np.isfinite(want[early:, :4]).all()
+    b.v[0][at, 1, 5] = 0.0
+    keep = b.new
+    res = owin.attend(f64(b.q)[:early], b.positions(0)[:early], f64(b.k[0]), f64(b.v[0]), np.arange(200))
+    compare(want[:early], f64(lse)[:early], res, 200, "rows before")
+    assert keep == b.new
+    b.kc[page, slot, 1] = float("nan")
+    o, lse = b.run()
+    compare(f64(o)[:early], f64(lse)[:early], res, 200, "rows before, K")
+    assert torch.isnan(o[early:, 4:]).all() and torch.isneginf(lse[early:, 4:]).all()
+
+
+def test_pages_that_name_nothing_read_as_zeros():
+    b = Batch([100, 64], [1, 1], 8, 2, seed=75, uniform=True)
+    b.tables[0, 1], b.tables[0, 3], b.tables[1, 0] = -1, b.n_blocks, 2**31 - 1
+    b.dev_tables.copy_(b.tables)
+    for s, p in ((0, 1), (0, 3), (1, 0)):
+        b.k[s][16 * p:16 * p + 16] = 0
+        b.v[s][16 * p:16 * p + 16] = 0
+    b.check(*b.run())
+
+
+def test_positions_beyond_the_table_read_as_zeros():
+    b = Batch([64], [1], 8, 2, seed=76, uniform=True, table_extra=0)
+    b.dev_len.fill_(100)
+    b.k[0] = torch.cat([b.k[0], torch.zeros(36, 2, D, dtype=torch.bfloat16)])
+    b.v[0] = torch.cat([b.v[0], torch.zeros(36, 2, D, dtype=torch.bfloat16)])
+    b.kv_len = [100]
+    b.check(*b.run())
+
+
+def test_scale_and_strided_queries():
+    b = Batch([77, 200, 9], [2, 2, 2], 8, 2, seed=77, uniform=True)
+    o, lse = b.run(scale=0.3)
+    b.check(o, lse, scale=0.3)
+    wide = torch.full((6, 8 + 4, D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wide[:, :8] = b.q.to(DEV)
+    got = torch.empty(6, 8, D, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(cp.attn_paged_workspace_size(b.kv, 6, 2, 8), dtype=torch.uint8, device=DEV)
+    cp.attn_paged(b.kv, wide[:, :8], got, ws, softmax_scale=0.3)  # no LSE
+    assert torch.equal(got, o)
+
+
+def test_large_scores_and_sinks():
+    """First tokens of far larger scores, and scores over a wide range."""
+    b = Batch([700], [3], 8, 2, seed=78, uniform=True)
+    b.k[0][:4] *= 12
+    b.k[0][100:] *= 4
+    starts = torch.tensor([0, 700], dtype=torch.int32, device=DEV)
+    cp.kv_append(b.kv, b.k[0].to(DEV), b.v[0].to(DEV), q_start=starts)
+    b.check(*b.run())
+    b.check(*b.run(64, 4), 64, 4)
+
+
+def test_repeated_calls_agree():
+    b = Batch([5000, 3, 900, 2500], [1, 1, 1, 1], 32, 8, seed=79, uniform=True)
+    first = b.run()
+    for _ in range(3):
+        again = b.run()
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_captured_launch_follows_the_lengths():
+    """One captured step (append, attend), replayed while lengths, tables and rows
+    change, against the eager calls."""
+    Hq, Hkv, n = 8, 2, 5
+    b = Batch([40, 1, 300, 17, 64], [1] * n, Hq, Hkv, seed=80, uniform=True, spare=200, table_extra=80)
+    free = [p for p in range(b.n_blocks) if p not in set(b.tables.flatten().tolist())]
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.empty(n, h, D, dtype=torch.bfloat16, device=DEV) for h in (Hq, Hkv, Hkv))
+    o, lse = torch.empty(n, Hq, D, dtype=torch.bfloat16, device=DEV), torch.empty(n, Hq, device=DEV)
+    ws = torch.empty(cp.attn_paged_workspace_size(b.kv, n, 1, Hq), dtype=torch.uint8, device=DEV)
+
+    def step():
+        cp.kv_append(b.kv, k, v)
+        cp.attn_paged(b.kv, q, o, ws, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        q.copy_(b.q.to(DEV)), k.zero_(), v.zero_()
+        step()  # (position kv_len - 1 is written again below)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn, add in enumerate([0, 1, 1, 40, 200]):
+        for s in range(n):
+            old, b.kv_len[s] = b.kv_len[s], b.kv_len[s] + add
+            b.k[s], b.v[s] = (torch.cat([x, randn(g, add, Hkv, D)]) for x in (b.k[s], b.v[s]))
+            for j in range(-(-old // B), -(-b.kv_len[s] // B)):
+                b.tables[s, j] = free.pop()
+        b.dev_tables.copy_(b.tables)
+        b.dev_len.copy_(torch.tensor(b.kv_len, dtype=torch.int32))
+        starts = torch.tensor(np.concatenate([[0], np.cumsum(b.kv_len)]), dtype=torch.int32, device=DEV)
+        cp.kv_append(b.kv, torch.cat(b.k).to(DEV), torch.cat(b.v).to(DEV), q_start=starts)
+        b.q = randn(g, n, Hq, D)
+        q.copy_(b.q.to(DEV))
+        k.copy_(torch.stack([x[-1] for x in b.k]).to(DEV))
+        v.copy_(torch.stack([x[-1] for x in b.v]).to(DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        b.check(o, lse)
+        got = o.clone()
+        step()
+        assert torch.equal(got, o), turn
+
+
+def test_another_stream():
+    b = Batch([500, 90], [1, 1], 8, 2, seed=81, uniform=True)
+    want = b.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = b.run()
+    side.synchronize()
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+# --- append ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("Hkv,head_dim", [(1, 128), (2, 128), (8, 128), (3, 40)])
+def test_append_positions(Hkv, head_dim):
+    """Ragged rows at odd positions, from a strided source; every other slot, and
+    rows outside the sequences, are left alone."""
+    g = torch.Generator().manual_seed(90 + Hkv)
+    kv_len, new = [5, 33, 16, 100, 4], [5, 7, 1, 0, 6]  # the last: two rows below position 0
+    tables = torch.randperm(40, generator=g)[:35].to(torch.int32).view(5, 7)
+    tables[1, 2] = -1   # position 32 has no page
+    start = np.cumsum([2] + new)
+    rows = int(start[-1]) + 3
+    fused = randn(g, rows, 2 * Hkv + 1, head_dim).to(DEV)
+    kc = randn(g, 40, B, Hkv, head_dim).to(DEV)
+    vc = randn(g, 40, B, Hkv, head_dim).to(DEV)
+    wk, wv = kc.clone(), vc.clone()
+    kv = cp.PagedKV(kc, vc, tables.to(DEV), torch.tensor(kv_len, dtype=torch.int32, device=DEV))
+    k, v = fused[:, 1:1 + Hkv], fused[:, 1 + Hkv:]
+    cp.kv_append(kv, k, v, q_start=torch.tensor(start, dtype=torch.int32, device=DEV))
+    for s in range(5):
+        for i in range(new[s]):
+            pos = kv_len[s] - new[s] + i
+            if pos >= 0 and tables[s, pos // B] >= 0:
+                wk[tables[s, pos // B], pos % B] = k[start[s] + i]
+                wv[tables[s, pos // B], pos % B] = v[start[s] + i]
+    assert torch.equal(kc, wk) and torch.equal(vc, wv)
+
+
+def test_append_past_the_table_is_passed_over():
+    kc, vc = (torch.zeros(8, B, 2, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    kv = cp.PagedKV(kc, vc, torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4),
+                    torch.tensor([70, 2**31 - 1], dtype=torch.int32, device=DEV))
+    rows = torch.ones(20, 2, D, dtype=torch.bfloat16, device=DEV)
+    cp.kv_append(kv, rows, rows)
+    want = torch.zeros_like(kc)
+    want[3, 12:] = 1  # positions 60 .. 63 of sequence 0
+    assert torch.equal(kc, want) and torch.equal(vc, want)
