@@ -20,7 +20,8 @@ LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 ARCH = "gfx950"
 
 SOURCES = ["plan.cpp", "cp_attn.cpp", "noalloc.cpp", "kv_cache.cpp", "attn_partial.hip", "lse_merge.hip",
-           "kv_cache.hip", "upload.hip", "attn_paged.cpp", "attn_rows.hip", "kv_pages.cpp", "kv_pages.hip"]
+           "kv_cache.hip", "upload.hip", "attn_paged.cpp", "attn_rows.hip", "attn_chunk.hip", "attn_merge.hip",
+           "kv_pages.cpp", "kv_pages.hip"]
 
 # Packed-FP32 VALU forms are kept out of every kernel (-packed-fp32-ops).
 HIP_FLAGS = [

@@ -1,0 +1,451 @@
+// Attention over a paged cache, or of a rank's rows through a window, of blocks of
+// many rows: chunks of prompts.  The mathematics, the rounding and the shares are
+// those of attn_rows.hip; what differs is what bounds it, the matrix cores.
+//
+// A workgroup of 8 waves (two per SIMD: one's vector work issues while the other's
+// products run) owns 128 NB rows of one KV head, 16 NB per wave, and walks their
+// keys in tiles of 32 that all waves read from LDS: every fragment of K or V that
+// is read feeds NB products.  One iteration runs O += V_{j-1}^T P_{j-1}, the
+// softmax of tile j and S_{j+1} = K_{j+1} Q^T as one sequence of 16 slots, each
+// with one fragment, its products and a share of the vector work; the loads of tile
+// j + kAhead go straight to LDS.  Weights are taken against the running maximum of
+// the tiles before, which needs no look at the tile's own scores: they stay exact
+// relative to each other at any size, so only a tile whose weights could
+// overflow is done again with its own maximum (as in attn_partial.hip).
+#include <hip/hip_runtime.h>
+
+#include "attn_tile.h"
+
+namespace cpattn {
+
+namespace {
+
+using namespace tile;
+
+constexpr int kWaves = kChunkThreads / 64;
+constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % kBufs
+constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
+constexpr int kSnap = 12;  // tiles: a part costs its set-up, and its rows a merge
+
+// LDS tiles by 16-byte columns: column c of a half holds chunk c of its 16 keys, key
+// k at slot k ^ 8 (c % 2).  The K reads (16 keys of a column) and the transposed V
+// reads (8 keys of two columns) touch every bank once, and the addresses of a
+// lane's fragments differ by constants.
+constexpr int kColBytes = kBlockTokens * 16;
+__device__ __forceinline__ int column_slot(int key, int c) { return c * kColBytes + ((key ^ (8 * (c & 1))) << 4); }
+
+struct Fragments {
+  uint32_t k, v;  // this lane's byte offsets in a K and in a V buffer
+};
+
+__device__ __forceinline__ bf16x8 load_k(const unsigned char* buf, const Fragments& f, int q) {  // q = 2 step + half
+  return *reinterpret_cast<const bf16x8*>(buf + f.k + (q & 1) * kHalfBytes + (q >> 1) * 4 * kColBytes);
+}
+__device__ __forceinline__ bf16x8 load_v(const unsigned char* buf, const Fragments& f, int db) {
+  typedef __attribute__((address_space(3))) s16x4* Lds;
+  const unsigned char* at = buf + f.v + db * 2 * kColBytes;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + kHalfBytes));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A direct-to-LDS load from a wave-uniform base plus this lane's offset.
+__device__ __forceinline__ void load_lds(const void* base, uint32_t off, uint32_t lds_base) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  const uint64_t bs = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+  asm volatile(
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1\n\t" ::"v"(off), "s"((const void*)(uintptr_t)bs),
+      "{m0}"(__builtin_amdgcn_readfirstlane((int)lds_base))
+      : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void pin(const T& x) {  // computed before this point of the schedule
+  asm volatile("" ::"v"(x));
+}
+
+template <int NB>
+using Scores = f32x4[NB][2];  // [block][half]
+
+template <int NB>
+struct Weights {
+  float sum[NB];     // fp32 sums of this lane's weights
+  bf16x2 pair[NB][4];
+};
+
+constexpr float kMaxSum = 65536.f;  // of a lane's 8 weights of a tile; beyond it is done again
+
+// One unit of a tile's softmax (of 12 NB, about equal): two exponentials of a pair
+// of scores, or the pair's rounding and sum.
+template <int NB>
+__device__ __forceinline__ void softmax_unit(int u, Scores<NB>& s, Weights<NB>& w, const float (&m)[NB], float sl2) {
+  const int b = u / 12, t = u % 12 / 3, kind = u % 3;  // block, pair
+
+
+  const int half = t >> 1, r = 2 * (t & 1);
+  if (kind < 2) {
+    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][half][r + kind], sl2, -m[b]));
+    pin(x);
+    s[b][half][r + kind] = x;
+  } else {
+    w.pair[b][t] = bf16x2{(__bf16)s[b][half][r], (__bf16)s[b][half][r + 1]};
+    w.sum[b] = t == 0 ? s[b][half][r] + s[b][half][r + 1] : w.sum[b] + (s[b][half][r] + s[b][half][r + 1]);
+    pin(w.sum[b]);
+    pin(w.pair[b][t]);
+  }
+}
+
+template <int NB>
+__device__ __forceinline__ void qk_step(Scores<NB>& s, const bf16x8& k, const bf16x8 (&qf)[NB][4], int q) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+    s[b][q & 1] = mfma16(k, qf[b][q >> 1], (q >> 1) == 0 ? f32x4{} : s[b][q & 1]);
+}
+
+template <int NB>
+__device__ __forceinline__ void qk_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&qf)[NB][4],
+                                        Scores<NB>& s) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) qk_step<NB>(s, load_k(buf, f, q), qf, q);
+}
+
+// Raises the running maxima to a tile's own where that is higher; O and the sums
+// follow.
+template <int NB>
+__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&psum)[NB],
+                                          f32x4 (&o)[8][NB], float sl2) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    float top = s[b][0][0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) top = __builtin_elementwise_maximum(top, s[b][r >> 2][r & 3]);
+    const float m_new = __builtin_elementwise_maximum(m[b], quad_max(top) * sl2);
+    const float alpha = __builtin_amdgcn_exp2f(m[b] - m_new);
+    l[b] *= alpha;
+    psum[b] *= alpha;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
+    m[b] = m_new;
+  }
+}
+
+// The weights become the operand of the second product.
+template <int NB>
+__device__ __forceinline__ void finish(const Weights<NB>& w, float (&l)[NB], bf16x8 (&pf)[NB]) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    l[b] += w.sum[b];
+    pf[b] = __builtin_shufflevector(__builtin_shufflevector(w.pair[b][0], w.pair[b][1], 0, 1, 2, 3),
+                                    __builtin_shufflevector(w.pair[b][2], w.pair[b][3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5,
+                                    6, 7);
+  }
+}
+
+template <int NB>
+__device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&pf)[NB],
+                                        f32x4 (&o)[8][NB]) {
+#pragma unroll
+  for (int db = 0; db < 8; ++db) {
+    const bf16x8 v = load_v(buf, f, db);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[db][b] = mfma16(v, pf[b], o[db][b]);
+  }
+}
+
+// The order of the units over an iteration: the exponentials of all blocks but the
+// last first, and the roundings from slot 8 on, when the products with the tile
+// before have freed their operand's registers.
+template <int NB>
+struct Order {
+  int unit[12 * NB];
+  constexpr Order() : unit{} {
+    int n = 0;
+    for (int b = 0; b + 1 < NB; ++b)
+      for (int t = 0; t < 4; ++t)
+        for (int k = 0; k < 2; ++k) unit[n++] = 12 * b + 3 * t + k;
+    const int last = 12 * (NB - 1);
+    int te = 0;
+    for (; n < 6 * NB; ++te)
+      for (int k = 0; k < 2; ++k) unit[n++] = last + 3 * te + k;
+    for (int b = 0; b + 1 < NB; ++b)
+      for (int t = 0; t < 4; ++t) unit[n++] = 12 * b + 3 * t + 2;
+    for (int t = 0; t < 4; ++t)
+      for (int k = t < te ? 2 : 0; k < 3; ++k) unit[n++] = last + 3 * t + k;
+  }
+};
+template <int NB>
+constexpr Order<NB> kOrder{};
+
+template <int NB>
+constexpr int kLookahead = NB == 2 ? 3 : 2;  // slots a fragment is read ahead of its products
+
+template <int NB>
+__global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParams p) {
+  // The buffers of K, of V, and a V tile of zeros.
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[(2 * kBufs + 1) * kTileBytes];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, i16 = lane & 15;
+  // Shares are numbered so that an XCD's workgroups (every eighth) have neighbouring
+  // ones, whose walks meet in its L2.
+  const int number = p.n_shares % 8 == 0 ? (int)(blockIdx.x % 8) * (p.n_shares / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
+  const Share share = find_share<kChunkThreads, 1, kSnap>(p, number);
+  if (tid == 0) p.starts[number] = share.at;
+  if (same(share.at, share.end)) return;
+
+  unsigned char* const kbuf = smem;
+  unsigned char* const vbuf = smem + kBufs * kTileBytes;
+  unsigned char* const vzero = smem + 2 * kBufs * kTileBytes;
+  static_assert(kTileBytes == 16 * kChunkThreads, "one 16-byte store per thread");
+  *reinterpret_cast<f32x4*>(vzero + 16 * tid) = f32x4{};
+  const Fragments fr = {(uint32_t)column_slot(i16, g),
+                        (uint32_t)(column_slot(4 * g + (i16 >> 2), (i16 & 3) >> 1) + 8 * (i16 & 1))};
+  // This wave's part of a tile's load: 1 KB of K and of V, four columns of one half.
+  const int load_half = wave >> 2;
+  const int load_key = i16 ^ (8 * (g & 1));
+  const int load_chunk = 4 * (wave & 3) + g;
+  const uint32_t load_off = (uint32_t)(load_key * p.kv_stride) + load_chunk * 16;
+  const uint32_t load_dst = lds_addr(smem) + load_half * kHalfBytes + (wave & 3) * 4 * kColBytes;
+  const float sl2 = p.scale_log2;
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
+
+  int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
+  int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
+  Segment s = segment_at(p, seg);
+  for (;;) {
+    const Walk w = block_walk(p, s, block);
+    const int n_steps = steps_of<1>(w);
+    const bool last = same_walk(share.end, ShareStart{seg, block, kvh, 0});
+    const int stop = last ? __builtin_amdgcn_readfirstlane(share.end.step) : n_steps;
+    const int n = w.n ? stop - step : 0;  // tiles of this part
+    const int rows = s.n * p.G, r0 = block * p.block_rows + 16 * NB * wave;
+    const bool active = r0 < rows && n > 0;  // a wave without rows only loads
+
+    int pos[NB];
+    bf16x8 qf[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      int r = r0 + 16 * b + i16;
+      r = r < rows ? r : rows - 1;
+      const int at = (int)((unsigned)r / (unsigned)p.G), h = r - at * p.G;
+      pos[b] = s.pos0 + at;
+      const uint16_t* q = p.q + (s.q_row + at) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
+    }
+    f32x4 o[8][NB], psum[NB];
+    float m[NB], l[NB];
+    bf16x8 pf[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
+      psum[b] = f32x4{};
+      pf[b] = bf16x8{};
+      m[b] = kNoMax;
+      l[b] = 0.f;
+    }
+
+    int ids = -1, ids_of = -64;  // pages of this wave's half of 64 tiles, one per lane
+    // Tile j of the part into buffer j % kBufs; past the last it is loaded again, into
+    // a buffer nobody reads, so that the waits can count.
+    auto load = [&](int j) {
+      const uint32_t dst = load_dst + (j & (kBufs - 1)) * kTileBytes;
+      const int jj = j < n ? j : n - 1;
+      const int t0 = tile_begin(w, step + jj);
+      const int hp = t0 + load_half * kBlockTokens;
+      if (__builtin_expect((jj & ~63) != ids_of, 0)) {
+        ids_of = jj & ~63;
+        ids = -1;
+        if (ids_of + lane < n) ids = page_of(p, s, tile_begin(w, step + ids_of + lane) + load_half * kBlockTokens);
+      }
+      const HalfSource h = half_source(p, __builtin_amdgcn_readlane(ids, jj & 63), hp, kvh);
+      const unsigned char* kb = (h.paged ? p.k_cache : p.k_new) + h.offset;
+      const unsigned char* vb = (h.paged ? p.v_cache : p.v_new) + h.offset;
+      if (__builtin_expect(whole_tile(w, t0) && !h.none, 1)) {
+        load_lds(kb, load_off, dst);
+        load_lds(vb, load_off, dst + kBufs * kTileBytes);
+      } else {
+        const bool read = !h.none && walked(w, hp + load_key);
+        const unsigned char* zeros = g_zeros + load_chunk * 16;
+        load_lds_from(read ? kb + load_off : zeros, dst);
+        load_lds_from(read ? vb + load_off : zeros, dst + kBufs * kTileBytes);
+      }
+    };
+    if (n > 0) {
+      __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the query fragments
+      for (int j = 0; j < kAhead; ++j) load(j);
+      int open0, open1;  // tiles of the walk that every row of the block sees whole
+      open_tiles(p, w, &open0, &open1);
+      int j = 0;
+#pragma unroll 1
+      while (j < n) {
+        // Tile j has landed for every wave, and the tiles before it have been read.
+        __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 1)));
+        __syncthreads();
+        const int j1 = open1 - step < n ? open1 - step : n;  // the end of the open tiles
+        const unsigned char* k_now = kbuf + (j & (kBufs - 1)) * kTileBytes;
+        const unsigned char* v_now = vbuf + (j & (kBufs - 1)) * kTileBytes;
+        Scores<NB> sa, sb;
+        Weights<NB> wt;
+        if (active) {
+          qk_tile<NB>(k_now, fr, qf, sa);
+          if (step + j < open0 || j >= j1) {
+            const int t0 = tile_begin(w, step + j);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mask_scores(p, sa[b], t0, g, pos[b]);
+          }
+          raise_max<NB>(sa, m, l, psum, o, sl2);
+        }
+        if (step + j < open0 || j >= j1) {
+          // A tile of which some row does not see every key, by itself.
+          load(j + kAhead);
+          if (active) {
+#pragma unroll
+            for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, sa, wt, m, sl2);
+            finish<NB>(wt, l, pf);
+            auto frag = [&](int db) { return load_v(v_now, fr, db); };
+            if (__builtin_expect(not_finite(frag), 0))
+              pv_not_finite<NB>(frag, pf, o);
+            else
+              pv_tile<NB>(v_now, fr, pf, o);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
+          }
+          ++j;
+          continue;
+        }
+        // Tiles j .. j1 - 1, pipelined.  No tile before the first: its V is zeros.
+        bf16x8 pre[kLookahead<NB>];
+        const unsigned char* v_before = vzero;
+        if (active) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) pf[b] = bf16x8{};
+#pragma unroll
+          for (int x = 0; x < kLookahead<NB>; ++x) pre[x] = load_v(vzero, fr, x);
+        }
+        auto iteration = [&](int j, Scores<NB>& s_in, Scores<NB>& s_out) {
+          const unsigned char* k_next = kbuf + ((j + 1) & (kBufs - 1)) * kTileBytes;
+          const unsigned char* v_this = vbuf + (j & (kBufs - 1)) * kTileBytes;
+          load(j + kAhead);
+          bf16x8 f[16];
+#pragma unroll
+          for (int x = 0; x < kLookahead<NB>; ++x) f[x] = pre[x];
+#pragma unroll
+          for (int slot = 0; slot < 16; ++slot) {
+            const int x = slot + kLookahead<NB>;
+            if (x < 8)
+              f[x] = load_v(v_before, fr, x);
+            else if (x < 16)
+              f[x] = load_k(k_next, fr, x - 8);
+            else
+              pre[x - 16] = load_v(v_this, fr, x - 16);
+            if (slot < 8) {
+#pragma unroll
+              for (int b = 0; b < NB; ++b) o[slot][b] = mfma16(f[slot], pf[b], o[slot][b]);
+              if (slot >= 2 && slot % 2 == 0 && (slot - 2) / 2 < NB)
+                psum[(slot - 2) / 2] = mfma16(ones, pf[(slot - 2) / 2], psum[(slot - 2) / 2]);
+            } else {
+              qk_step<NB>(s_out, f[slot], qf, slot - 8);
+            }
+#pragma unroll
+            for (int u = slot * 12 * NB / 16; u < (slot + 1) * 12 * NB / 16; ++u)
+              softmax_unit<NB>(kOrder<NB>.unit[u], s_in, wt, m, sl2);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          bool fine = true;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) fine = fine && wt.sum[b] <= kMaxSum;
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
+            qk_tile<NB>(kbuf + (j & (kBufs - 1)) * kTileBytes, fr, qf, s_in);
+            raise_max<NB>(s_in, m, l, psum, o, sl2);
+#pragma unroll
+            for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, s_in, wt, m, sl2);
+          }
+          finish<NB>(wt, l, pf);
+          v_before = v_this;
+        };
+        // In pairs behind one barrier (the first pair's is above): at a pair's start
+        // every tile up to j + 2 has landed, and the buffers that its loads fill were
+        // last read before it.
+        if (active) {
+          for (;;) {
+            __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
+            __syncthreads();
+            iteration(j, sa, sb);
+            if (++j >= j1) break;
+            iteration(j, sb, sa);
+            if (++j >= j1) break;
+          }
+          pv_tile<NB>(v_before, fr, pf, o);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
+        } else {
+          for (;;) {
+            __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
+            __syncthreads();
+            load(j + kAhead);
+            if (++j >= j1) break;
+            load(j + kAhead);
+            if (++j >= j1) break;
+          }
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no load may still be writing LDS
+    }
+
+    const bool part = step > 0 || stop < n_steps;
+    float* slot = p.slots + (2 * (size_t)number + (step > 0 ? 0 : 1)) * slot_floats(p.block_rows);
+    if (r0 < rows)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int r = r0 + 16 * b + i16;
+        const float sum = quad_sum(l[b]), rounded = psum[b][0];
+        const bool live = m[b] > 0.5f * kNoMax && sum > 0.f;
+        const float inv = live ? 1.f / rounded : (sum != sum ? sum : 0.f);
+        const float lse = live ? m[b] * kLn2 + logf(sum) : -INFINITY;
+        if (part) {
+          const int rb = 16 * (NB * wave + b) + i16;
+#pragma unroll
+          for (int db = 0; db < 8; ++db)
+            *reinterpret_cast<f32x4*>(slot + rb * kHeadDim + 16 * db + 4 * g) = o[db][b] * inv;
+          if (g == 0) slot[p.block_rows * kHeadDim + rb] = sum != sum ? sum : lse;
+        } else if (r < rows) {
+          const int at = (int)((unsigned)r / (unsigned)p.G);
+          const int64_t out = (s.o_row + at) * p.Hq + kvh * p.G + (r - at * p.G);
+#pragma unroll
+          for (int db = 0; db < 8; ++db) {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            bf16x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[db][b][e] * inv);
+            *reinterpret_cast<bf16x4*>(p.o + out * kHeadDim + 16 * db + 4 * g) = v;
+          }
+          if (g == 0 && p.lse) p.lse[out] = lse;
+        }
+      }
+    if (last) return;
+    step = 0;
+    if (!next_walk(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
+    __syncthreads();  // every wave is done with the buffers
+  }
+}
+
+}  // namespace
+
+int launch_attn_chunk(const PagedParams& p, void* stream, const char* who) {
+  const dim3 grid((unsigned)p.n_shares), block(kChunkThreads);
+  if (p.block_rows == 16 * kWaves * 2)
+    hipLaunchKernelGGL(attn_chunk_kernel<2>, grid, block, 0, (hipStream_t)stream, p);
+  else
+    hipLaunchKernelGGL(attn_chunk_kernel<3>, grid, block, 0, (hipStream_t)stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));
+  return launch_attn_merge(p, stream, who);
+}
+
+}  // namespace cpattn

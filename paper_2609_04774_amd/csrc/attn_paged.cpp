@@ -40,10 +40,12 @@ int set_common(PagedParams* p, const std::string& who, int32_t Hq, int32_t Hkv, 
   return CP_OK;
 }
 
-// Rows of a block: the fewest that hold the most rows of a sequence and KV head.
+// Rows of a block: the fewest that hold the most rows of a sequence and KV head, up to
+// 64 with the kernel of few rows; else those of the other.
+constexpr int kChunkRows = 256;
 int block_rows(int64_t max_q, int32_t G) {
   const int64_t rows = max_q * G;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : kChunkRows;
 }
 
 size_t starts_bytes() { return ((size_t)kShares * sizeof(ShareStart) + 255) / 256 * 256; }
@@ -62,7 +64,8 @@ int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspac
   p->block_rows = block_rows(max_q, p->G);
   p->starts = static_cast<ShareStart*>(workspace);
   p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes());
-  return launch_attn_rows(*p, stream, who.substr(0, who.size() - 2).c_str());
+  const std::string name = who.substr(0, who.size() - 2);
+  return p->block_rows == kChunkRows ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
 }
 
 // The most rows of a sequence, from a batch's arguments.

@@ -15,7 +15,7 @@
 // one per workgroup and compute unit, wherever the cut falls (the lengths are
 // read from the device, so that a captured launch follows them): no unit waits
 // for another's longer sequence.  A part that ends inside a walk leaves a partial
-// result, and rows_merge_kernel combines a walk's.  Each of a workgroup's four
+// result, and share_merge_kernel combines a walk's.  Each of a workgroup's four
 // waves takes every fourth tile of 32 keys into its own LDS (two tiles of K and of
 // V, loaded directly, the next ones in flight while one is used), so the waves
 // meet only at the end of a walk.
@@ -32,87 +32,6 @@ using namespace tile;
 constexpr int kWaves = kRowsThreads / 64;
 constexpr int kWaveBytes = 4 * kTileBytes;  // two K tiles, two V tiles
 constexpr int kLoads = kTileBytes / 1024;   // direct-to-LDS loads of a tile and tensor, 1 KB each
-
-__device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
-  return (int)(((int64_t)n * p.G + p.block_rows - 1) / p.block_rows);
-}
-
-__device__ __forceinline__ Walk block_walk(const PagedParams& p, const Segment& s, int block) {
-  const int r0 = block * p.block_rows;
-  const int rows = s.n * p.G;
-  return walk_of(p, s, r0, r0 + p.block_rows < rows ? r0 + p.block_rows : rows);
-}
-
-// Steps of a walk; one at least, which stores the rows of a block without keys.
-__device__ __forceinline__ int steps_of(const Walk& w) {
-  const int n = (w.n + kWaves - 1) / kWaves;
-  return n > 0 ? n : 1;
-}
-
-__device__ __forceinline__ int64_t segment_steps(const PagedParams& p, int s) {
-  const Segment x = segment_at(p, s);
-  int64_t n = 0;
-  for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) n += steps_of(block_walk(p, x, b));
-  return n;
-}
-
-// The start of this workgroup's share and its length in steps.  Every thread
-// counts the steps of its run of segments, and a scan finds the one that the
-// share begins in.  The heads of a block follow one another: neighbouring
-// workgroups read the same pages.
-struct Share {
-  ShareStart at;
-  int64_t n;
-};
-
-__device__ Share find_share(const PagedParams& p, int share) {
-  __shared__ int64_t wave_sum[kWaves];
-  __shared__ Share found;
-  const int tid = threadIdx.x;
-  const int per = (p.n_segments + kRowsThreads - 1) / kRowsThreads;
-  const int s0 = tid * per < p.n_segments ? tid * per : p.n_segments;
-  const int s1 = s0 + per < p.n_segments ? s0 + per : p.n_segments;
-  int64_t mine = 0;
-  for (int s = s0; s < s1; ++s) mine += segment_steps(p, s);
-  int64_t before = mine;
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) {
-    const int64_t x = __shfl_up(before, k);
-    if ((tid & 63) >= k) before += x;
-  }
-  if ((tid & 63) == 63) wave_sum[tid >> 6] = before;
-  if (tid == 0) found = Share{{0, 0, 0, 0}, 0};
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < (tid >> 6)) before += wave_sum[w];
-    total += wave_sum[w];
-  }
-  before -= mine;
-  total *= p.Hkv;
-  // No share between two others is empty: with fewer steps the last ones are.
-  const int64_t n = total < p.n_shares ? total : p.n_shares;
-  const int64_t u0 = share < n ? total * share / n : total, u1 = share < n ? total * (share + 1) / n : total;
-  if (u1 > u0 && u0 >= before * p.Hkv && u0 < (before + mine) * p.Hkv) {
-    int64_t u = u0 - before * p.Hkv;
-    for (int s = s0; s < s1; ++s) {
-      const Segment x = segment_at(p, s);
-      for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) {
-        const int n = steps_of(block_walk(p, x, b));
-        if (u < (int64_t)n * p.Hkv) {
-          if (u >= 0) found = Share{{s, b, (int)(u / n), (int)(u % n)}, u1 - u0};
-          u = -1;
-          s = s1;
-          break;
-        }
-        u -= (int64_t)n * p.Hkv;
-      }
-    }
-  }
-  __syncthreads();
-  return found;
-}
 
 // One tile's loads of K (tensor 0) or V: 1 KB each, four keys of 256 bytes.  `off`
 // are this lane's offsets within a half (four loads of it).
@@ -143,9 +62,9 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
-  const Share share = find_share(p, blockIdx.x);
-  if (tid == 0) p.starts[blockIdx.x] = share.n ? share.at : ShareStart{-1, 0, 0, 0};
-  if (share.n == 0) return;
+  const Share share = find_share<kRowsThreads, kWaves, 1>(p, blockIdx.x);
+  if (tid == 0) p.starts[blockIdx.x] = share.at;
+  if (same(share.at, share.end)) return;
 
   unsigned char* const mine = smem + wave * kWaveBytes;
   const uint32_t lds = lds_addr(mine);
@@ -161,12 +80,12 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
 
   int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
   int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
-  int64_t left = share.n;
   Segment s = segment_at(p, seg);
   for (;;) {
     const Walk w = block_walk(p, s, block);
-    const int n_steps = steps_of(w);
-    const int stop = left < n_steps - step ? step + (int)left : n_steps;
+    const int n_steps = steps_of<kWaves>(w);
+    const bool last = same_walk(share.end, ShareStart{seg, block, kvh, 0});
+    const int stop = last ? share.end.step : n_steps;
     const int rows = s.n * p.G, r0 = block * p.block_rows;
 
     // Rows past the block's end repeat its last one and are not stored.
@@ -274,8 +193,9 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       __builtin_amdgcn_s_waitcnt(wait_vm(3 * kLoads));  // V of tile j
       asm volatile("" ::: "memory");
       // Keys hidden from every row are zeros; hidden from some, they may be anything.
-      if (__builtin_expect(!open && w.p_lo != w.p_hi && not_finite(vt, lane), 0)) {
-        pv_not_finite<NB>(vt, lane, pf, o);
+      auto frag = [&](int db) { return v_frag(vt, lane, db); };
+      if (__builtin_expect(!open && w.p_lo != w.p_hi && not_finite(frag), 0)) {
+        pv_not_finite<NB>(frag, pf, o);
       } else {
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
@@ -348,89 +268,11 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
         if (c == 0 && p.lse) p.lse[out] = lse;
       }
     }
-    left -= stop - step;
-    if (left <= 0) return;
-    __syncthreads();  // the LDS is free for the next walk's tiles
+    if (last) return;
     step = 0;
-    if (++kvh == p.Hkv) {
-      kvh = 0;
-      ++block;
-      while (block >= blocks_of(p, s.n)) {
-        block = 0;
-        if (++seg >= p.n_segments) return;  // (never: a share ends with the last walk)
-        s = segment_at(p, seg);
-      }
-    }
+    if (!next_walk(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
+    __syncthreads();  // the LDS is free for the next walk's tiles
   }
-}
-
-// The parts of a walk that was cut, combined (they cover disjoint keys): LSE = M +
-// ln sum_k e^{LSE_k - M}, O = sum_k e^{LSE_k - LSE} O_k.  A walk's first part is
-// the second slot of the share that it begins in, the others are the first slots of
-// the shares that begin within it.  Block (x, y): the walk that share x begins
-// within, if it is the first to do so, rows 4 y .. 4 y + 3, one wave each.
-__global__ __launch_bounds__(256) void rows_merge_kernel(PagedParams p) {
-  const int share = blockIdx.x + 1;
-  const ShareStart at = p.starts[share];
-  if (at.segment < 0 || at.step == 0) return;
-  auto same = [&](const ShareStart& x) { return x.segment == at.segment && x.block == at.block && x.kvh == at.kvh; };
-  if (share > 1) {
-    const ShareStart before = p.starts[share - 1];
-    if (same(before) && before.step > 0) return;
-  }
-  const Segment s = segment_at(p, at.segment);
-  const int lane = threadIdx.x & 63;
-  const int r = 4 * blockIdx.y + (threadIdx.x >> 6);
-  const int row = at.block * p.block_rows + r;
-  if (r >= p.block_rows || row >= s.n * p.G) return;
-  const size_t size = slot_floats(p.block_rows);
-  // The walk's shares: this one and those after it that begin within the walk.
-  int n = 1;
-  for (;; n += 64) {
-    const int k = share + n + lane;
-    bool in = k < p.n_shares;
-    if (in) {
-      const ShareStart x = p.starts[k];
-      in = same(x) && x.step > 0;
-    }
-    const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
-    if (mask != ~0ull) {
-      n += __builtin_ctzll(~mask);
-      break;
-    }
-  }
-  // Part 0 lies in the share before; part k in share + k - 1.
-  auto slot_of = [&](int k) { return p.slots + (2 * (size_t)(share - 1 + k) + (k == 0 ? 1 : 0)) * size; };
-  auto lse_of = [&](int k) { return slot_of(k)[(size_t)p.block_rows * kHeadDim + r]; };
-  float top = -INFINITY;
-  for (int k = lane; k <= n; k += 64) top = __builtin_elementwise_maximum(top, lse_of(k));
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) top = __builtin_elementwise_maximum(top, __shfl_xor(top, k));
-  float2 acc = make_float2(0.f, 0.f);
-  float sum = 0.f;
-  if (top != -INFINITY) {
-    for (int k0 = 0; k0 <= n; k0 += 64) {
-      const float l = k0 + lane <= n ? lse_of(k0 + lane) : -INFINITY;
-      const float w = l == -INFINITY ? 0.f : expf(l - top);
-      sum += w;
-      const int end = n + 1 - k0 < 64 ? n + 1 - k0 : 64;
-      for (int k = 0; k < end; ++k) {
-        const float wk = __shfl(w, k);
-        const float2 v = reinterpret_cast<const float2*>(slot_of(k0 + k) + (size_t)r * kHeadDim)[lane];
-        acc.x += wk * v.x;
-        acc.y += wk * v.y;
-      }
-    }
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
-    acc.x /= sum;
-    acc.y /= sum;
-  }
-  const int i = (int)((unsigned)row / (unsigned)p.G);
-  const int64_t out = (s.o_row + i) * p.Hq + at.kvh * p.G + (row - i * p.G);
-  const bf16x2 v = {(__bf16)acc.x, (__bf16)acc.y};
-  reinterpret_cast<bf16x2*>(p.o + out * kHeadDim)[lane] = v;
-  if (lane == 0 && p.lse) p.lse[out] = top == top && top != -INFINITY ? top + logf(sum) : -INFINITY;
 }
 
 int launched(const char* who) {
@@ -449,10 +291,8 @@ int launch_attn_rows(const PagedParams& p, void* stream, const char* who) {
     hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);
   else
     hipLaunchKernelGGL(attn_rows_kernel<4>, grid, block, 0, st, p);
-  int rc = launched(who);
-  if (rc != CP_OK || p.n_shares == 1) return rc;
-  hipLaunchKernelGGL(rows_merge_kernel, dim3((unsigned)p.n_shares - 1, (unsigned)(p.block_rows / 4)), dim3(256), 0, st, p);
-  return launched(who);
+  const int rc = launched(who);
+  return rc == CP_OK ? launch_attn_merge(p, stream, who) : rc;
 }
 
 }  // namespace cpattn

@@ -120,6 +120,127 @@ __device__ __forceinline__ bool open_tile(const PagedParams& p, const Walk& w, i
          (!p.window || t0 > w.p_hi - p.window || t0 + kTileKeys <= p.n_sink);
 }
 
+// The run [*first, *end) of tiles that every row sees whole (sink tiles aside).
+__device__ __forceinline__ void open_tiles(const PagedParams& p, const Walk& w, int* first, int* end) {
+  const int below = p.window ? w.p_hi - p.window + 1 - w.base : 0;  // keys from base on that some row does not see
+  const int a = w.n_sink_tiles + (below > 0 ? (below + kTileKeys - 1) / kTileKeys : 0);
+  const int keys = w.p_lo + 1 - w.base;
+  const int b = w.n_sink_tiles + (keys > 0 ? keys / kTileKeys : 0);
+  *first = a < w.n ? a : w.n;
+  *end = b > *first ? b : *first;
+}
+
+// ---------------------------------------------------------------------------
+// Shares.  The walks of all blocks of rows -- in the order segment, block, KV head
+// (the heads of a block follow one another: neighbouring workgroups read the same
+// pages) -- are counted in steps of kTiles tiles and cut into equal shares, one per
+// workgroup.
+
+__device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
+  return (int)(((int64_t)n * p.G + p.block_rows - 1) / p.block_rows);
+}
+
+__device__ __forceinline__ Walk block_walk(const PagedParams& p, const Segment& s, int block) {
+  const int r0 = block * p.block_rows;
+  const int rows = s.n * p.G;
+  return walk_of(p, s, r0, r0 + p.block_rows < rows ? r0 + p.block_rows : rows);
+}
+
+// Steps of a walk; one at least, which stores the rows of a block without keys.
+template <int kTiles>
+__device__ __forceinline__ int steps_of(const Walk& w) {
+  const int n = (w.n + kTiles - 1) / kTiles;
+  return n > 0 ? n : 1;
+}
+
+__device__ __forceinline__ bool same_walk(const ShareStart& a, const ShareStart& b) {
+  return a.segment == b.segment && a.block == b.block && a.kvh == b.kvh;
+}
+__device__ __forceinline__ bool same(const ShareStart& a, const ShareStart& b) { return same_walk(a, b) && a.step == b.step; }
+
+// The walk after this one; false behind the last.
+__device__ __forceinline__ bool next_walk(const PagedParams& p, Segment* s, int* seg, int* block, int* kvh) {
+  if (++*kvh < p.Hkv) return true;
+  *kvh = 0;
+  ++*block;
+  while (*block >= blocks_of(p, s->n)) {
+    *block = 0;
+    if (++*seg >= p.n_segments) return false;
+    *s = segment_at(p, *seg);
+  }
+  return true;
+}
+
+// A share is [at, end); behind the last walk is segment n_segments.  Each is a step
+// of a walk, or the start of one: a cut less than kSnap steps from a walk's start or
+// end moves there (a shorter part costs more than it evens out).
+struct Share {
+  ShareStart at, end;
+};
+
+// Every thread counts the steps of its run of segments, and a scan finds the walk of
+// each of the share's two ends.
+template <int kThreads, int kTiles, int kSnap>
+__device__ Share find_share(const PagedParams& p, int share) {
+  __shared__ int64_t wave_sum[kThreads / 64];
+  __shared__ ShareStart found[2];
+  const int tid = threadIdx.x;
+  const int per = (p.n_segments + kThreads - 1) / kThreads;
+  const int s0 = tid * per < p.n_segments ? tid * per : p.n_segments;
+  const int s1 = s0 + per < p.n_segments ? s0 + per : p.n_segments;
+  int64_t mine = 0;
+  for (int s = s0; s < s1; ++s) {
+    const Segment x = segment_at(p, s);
+    for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) mine += steps_of<kTiles>(block_walk(p, x, b));
+  }
+  int64_t before = mine;
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    const int64_t x = __shfl_up(before, k);
+    if ((tid & 63) >= k) before += x;
+  }
+  if ((tid & 63) == 63) wave_sum[tid >> 6] = before;
+  if (tid < 2) found[tid] = ShareStart{p.n_segments, 0, 0, 0};
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < (tid >> 6)) before += wave_sum[w];
+    total += wave_sum[w];
+  }
+  before -= mine;
+  total *= p.Hkv;
+  // With fewer steps than shares the last shares are empty.
+  const int64_t n = total < p.n_shares ? total : p.n_shares;
+  for (int e = 0; e < 2; ++e) {
+    if (share + e >= n) continue;
+    int64_t u = total * (share + e) / n - before * p.Hkv;
+    if (u < 0 || u >= mine * p.Hkv) continue;
+    for (int s = s0; s < s1 && u >= 0; ++s) {
+      const Segment x = segment_at(p, s);
+      for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) {
+        const int steps = steps_of<kTiles>(block_walk(p, x, b));
+        if (u >= (int64_t)steps * p.Hkv) {
+          u -= (int64_t)steps * p.Hkv;
+          continue;
+        }
+        int seg = s, block = b, kvh = (int)(u / steps), step = (int)(u % steps);
+        if (step < kSnap) step = 0;
+        if (step && steps - step < kSnap) {
+          Segment y = x;
+          step = 0;
+          if (!next_walk(p, &y, &seg, &block, &kvh)) seg = p.n_segments, block = kvh = 0;
+        }
+        found[e] = ShareStart{seg, block, kvh, step};
+        u = -1;
+        break;
+      }
+    }
+  }
+  __syncthreads();
+  return Share{found[0], found[1]};
+}
+
 // ---------------------------------------------------------------------------
 // K and V tiles in LDS.  A half is one page's 16 keys of one KV head, 256 bytes
 // each; 16-byte chunk c of key k (of the half) lies at slot c ^ swizzle(k) of the
@@ -225,12 +346,14 @@ __device__ __forceinline__ void mask_scores(const PagedParams& p, f32x4 (&s)[2],
     }
 }
 
-// Whether the V tile holds an infinity or a NaN: its product with zeros is not 0.
-__device__ __forceinline__ bool not_finite(const unsigned char* v, int lane) {
+// Whether a V tile (its fragments v(db)) holds an infinity or a NaN: its product with
+// zeros is not 0.
+template <class Frag>
+__device__ __forceinline__ bool not_finite(Frag&& v) {
   f32x4 z = {};
   bf16x8 zeros = {};
 #pragma unroll
-  for (int db = 0; db < 8; ++db) z = mfma16(v_frag(v, lane, db), zeros, z);
+  for (int db = 0; db < 8; ++db) z = mfma16(v(db), zeros, z);
   const bool bad = !(z[0] == 0.f && z[1] == 0.f && z[2] == 0.f && z[3] == 0.f);
   return __builtin_amdgcn_ballot_w64(bad) != 0;
 }
@@ -238,38 +361,39 @@ __device__ __forceinline__ bool not_finite(const unsigned char* v, int lane) {
 // O^T += V^T P^T of such a tile, where some of its keys are hidden from some rows
 // of the block: a weight of 0 times an infinity would be a NaN.  The finite values
 // are added as ever; a row takes the others from the keys that it sees.
-template <int NB>
-__device__ __forceinline__ void pv_not_finite(const unsigned char* v, int lane, const bf16x8 (&pf)[NB],
-                                              f32x4 (&o)[8][NB]) {
+template <int NB, class Frag>
+__device__ __forceinline__ void pv_not_finite(Frag&& v, const bf16x8 (&pf)[NB], f32x4 (&o)[8][NB]) {
+  // (One fragment at a time: this rare path has to leave registers to the common one.)
+  auto products = [&](auto&& of_value, auto&& use) {
 #pragma unroll
-  for (int db = 0; db < 8; ++db) {
-    const bf16x8 f = v_frag(v, lane, db);
-    bf16x8 fine, up, down, nan;
+    for (int db = 0; db < 8; ++db) {
+      bf16x8 f = v(db);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = (float)f[e];
-      fine[e] = (__bf16)(__builtin_isfinite(x) ? x : 0.f);
-      up[e] = (__bf16)(x == INFINITY ? 1.f : 0.f);
-      down[e] = (__bf16)(x == -INFINITY ? 1.f : 0.f);
-      nan[e] = (__bf16)(x != x ? 1.f : 0.f);
+      for (int e = 0; e < 8; ++e) f[e] = (__bf16)of_value((float)f[e]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) use(db, b, f);
       __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  auto count_seen = [&](int b, const bf16x8& f) {
+    bf16x8 seen;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      bf16x8 seen;
+    for (int e = 0; e < 8; ++e) seen[e] = (__bf16)((float)pf[b][e] == 0.f ? 0.f : 1.f);
+    return mfma16(f, seen, f32x4{});
+  };
+  products([](float x) { return __builtin_isfinite(x) ? x : 0.f; },
+           [&](int db, int b, const bf16x8& f) { o[db][b] = mfma16(f, pf[b], o[db][b]); });
+  auto add = [&](auto&& is, float what) {
+    products([&](float x) { return is(x) ? 1.f : 0.f; },
+             [&](int db, int b, const bf16x8& f) {
+               const f32x4 n = count_seen(b, f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) seen[e] = (__bf16)((float)pf[b][e] == 0.f ? 0.f : 1.f);
-      o[db][b] = mfma16(fine, pf[b], o[db][b]);
-      const f32x4 a = mfma16(up, seen, f32x4{}), c = mfma16(down, seen, f32x4{}), n = mfma16(nan, seen, f32x4{});
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (a[r] > 0.f) o[db][b][r] += INFINITY;
-        if (c[r] > 0.f) o[db][b][r] -= INFINITY;
-        if (n[r] > 0.f) o[db][b][r] = NAN;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
+               for (int r = 0; r < 4; ++r) o[db][b][r] += n[r] > 0.f ? what : 0.f;
+             });
+  };
+  add([](float x) { return x == INFINITY; }, INFINITY);
+  add([](float x) { return x == -INFINITY; }, -INFINITY);
+  add([](float x) { return x != x; }, NAN);
 }
 
 }  // namespace tile

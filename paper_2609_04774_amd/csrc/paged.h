@@ -59,11 +59,14 @@ struct ShareStart {
 };
 
 constexpr int kRowsThreads = 256;
+constexpr int kChunkThreads = 512;
 constexpr int kShares = 256;  // one workgroup per compute unit
 
 __host__ __device__ constexpr size_t slot_floats(int rows) { return (size_t)rows * (kHeadDim + 1); }
 
 int launch_attn_rows(const PagedParams& p, void* stream, const char* who);
+int launch_attn_chunk(const PagedParams& p, void* stream, const char* who);
+int launch_attn_merge(const PagedParams& p, void* stream, const char* who);
 
 // ---------------------------------------------------------------------------
 // The pages of a cache.
