@@ -470,8 +470,8 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  *               dense; else a multiple of 8, at least n_heads_q * 128).
  *   q_start     as above, or NULL (n_rows % n_seqs == 0).
  *   max_q       the most rows of a sequence (ignored with q_start NULL).  Rows of
- *               a sequence past it are left as they were.  Up to 64 (row, query
- *               head) pairs per KV head take kernels for few rows.
+ *               a sequence past it are left as they were.  Up to 32 (row, query
+ *               head) pairs per KV head take a kernel for few rows.
  *   n_heads_q   a multiple of n_heads_kv; head_dim 128.
  *   softmax_scale  <= 0 selects 1/sqrt(head_dim).
  *   window      keys visible behind a row, itself included; 0: all.

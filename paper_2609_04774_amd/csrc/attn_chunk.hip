@@ -25,6 +25,7 @@ using namespace tile;
 constexpr int kWaves = kChunkThreads / 64;
 constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % kBufs
 constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
+constexpr int kSetup = 10;  // of a walk, in tiles
 constexpr int kSnap = 12;  // tiles: a part costs its set-up, and its rows a merge
 
 // LDS tiles by 16-byte columns: column c of a half holds chunk c of its 16 keys, key
@@ -114,8 +115,7 @@ __device__ __forceinline__ void qk_tile(const unsigned char* buf, const Fragment
 // Raises the running maxima to a tile's own where that is higher; O and the sums
 // follow.
 template <int NB>
-__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&psum)[NB],
-                                          f32x4 (&o)[8][NB], float sl2) {
+__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     float top = s[b][0][0];
@@ -124,7 +124,6 @@ __device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], f
     const float m_new = __builtin_elementwise_maximum(m[b], quad_max(top) * sl2);
     const float alpha = __builtin_amdgcn_exp2f(m[b] - m_new);
     l[b] *= alpha;
-    psum[b] *= alpha;
 #pragma unroll
     for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
     m[b] = m_new;
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   // Shares are numbered so that an XCD's workgroups (every eighth) have neighbouring
   // ones, whose walks meet in its L2.
   const int number = p.n_shares % 8 == 0 ? (int)(blockIdx.x % 8) * (p.n_shares / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
-  const Share share = find_share<kChunkThreads, 1, kSnap>(p, number);
+  const Share share = find_share<kChunkThreads, 1, kSetup, kSnap, true>(p, number);
   if (tid == 0) p.starts[number] = share.at;
   if (same(share.at, share.end)) return;
 
@@ -209,18 +208,20 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   const uint32_t load_off = (uint32_t)(load_key * p.kv_stride) + load_chunk * 16;
   const uint32_t load_dst = lds_addr(smem) + load_half * kHalfBytes + (wave & 3) * 4 * kColBytes;
   const float sl2 = p.scale_log2;
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
 
-  int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
-  int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
+  // The start of the share's last walk comes first, then the end of its first walk,
+  // then the walks between: the workgroups of an XCD, whose shares are cut at any
+  // place of walks over the same keys, so pass over the keys together.
+  const ShareStart at = uniform(share.at), end = uniform(share.end);
+  bool ahead = end.step > 0 && !same_walk(at, end);
+  int seg = ahead ? end.segment : at.segment, block = ahead ? end.block : at.block, kvh = ahead ? end.kvh : at.kvh;
   Segment s = segment_at(p, seg);
   for (;;) {
     const Walk w = block_walk(p, s, block);
     const int n_steps = steps_of<1>(w);
-    const bool last = same_walk(share.end, ShareStart{seg, block, kvh, 0});
-    const int stop = last ? __builtin_amdgcn_readfirstlane(share.end.step) : n_steps;
+    const ShareStart here = {seg, block, kvh, 0};
+    const int step = same_walk(here, at) ? at.step : 0;
+    const int stop = same_walk(here, end) ? end.step : n_steps;
     const int n = w.n ? stop - step : 0;  // tiles of this part
     const int rows = s.n * p.G, r0 = block * p.block_rows + 16 * NB * wave;
     const bool active = r0 < rows && n > 0;  // a wave without rows only loads
@@ -237,14 +238,13 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
 #pragma unroll
       for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
     }
-    f32x4 o[8][NB], psum[NB];
+    f32x4 o[8][NB];
     float m[NB], l[NB];
     bf16x8 pf[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
-      psum[b] = f32x4{};
       pf[b] = bf16x8{};
       m[b] = kNoMax;
       l[b] = 0.f;
@@ -281,45 +281,49 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
       for (int j = 0; j < kAhead; ++j) load(j);
       int open0, open1;  // tiles of the walk that every row of the block sees whole
       open_tiles(p, w, &open0, &open1);
+      auto closed = [&](int j) { return (step + j < open0) | (step + j >= open1); };
+      auto mask = [&](int j, Scores<NB>& sc) {
+        if (__builtin_expect(!closed(j), 1)) return;
+        const int t0 = tile_begin(w, step + j);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) mask_scores(p, sc[b], t0, g, pos[b]);
+      };
+      // A tile with keys that some row does not see, and an infinity or a NaN in V (a
+      // weight of 0 times it would be a NaN): taken by itself.  Every wave looks at the
+      // same values.
+      auto apart = [&](int j) {
+        if (__builtin_expect(!closed(j), 1)) return false;
+        const unsigned char* v = vbuf + (j & (kBufs - 1)) * kTileBytes;
+        return not_finite([&](int db) { return load_v(v, fr, db); });
+      };
       int j = 0;
 #pragma unroll 1
       while (j < n) {
         // Tile j has landed for every wave, and the tiles before it have been read.
         __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 1)));
         __syncthreads();
-        const int j1 = open1 - step < n ? open1 - step : n;  // the end of the open tiles
         const unsigned char* k_now = kbuf + (j & (kBufs - 1)) * kTileBytes;
         const unsigned char* v_now = vbuf + (j & (kBufs - 1)) * kTileBytes;
         Scores<NB> sa, sb;
         Weights<NB> wt;
         if (active) {
           qk_tile<NB>(k_now, fr, qf, sa);
-          if (step + j < open0 || j >= j1) {
-            const int t0 = tile_begin(w, step + j);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) mask_scores(p, sa[b], t0, g, pos[b]);
-          }
-          raise_max<NB>(sa, m, l, psum, o, sl2);
+          mask(j, sa);
+          raise_max<NB>(sa, m, l, o, sl2);
         }
-        if (step + j < open0 || j >= j1) {
-          // A tile of which some row does not see every key, by itself.
+        if (__builtin_expect(apart(j), 0)) {
           load(j + kAhead);
           if (active) {
 #pragma unroll
             for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, sa, wt, m, sl2);
             finish<NB>(wt, l, pf);
-            auto frag = [&](int db) { return load_v(v_now, fr, db); };
-            if (__builtin_expect(not_finite(frag), 0))
-              pv_not_finite<NB>(frag, pf, o);
-            else
-              pv_tile<NB>(v_now, fr, pf, o);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
+            pv_not_finite<NB>([&](int db) { return load_v(v_now, fr, db); }, pf, o);
           }
           ++j;
           continue;
         }
-        // Tiles j .. j1 - 1, pipelined.  No tile before the first: its V is zeros.
+        // The tiles up to the next such one, pipelined.  No tile before the first: its V
+        // is zeros.
         bf16x8 pre[kLookahead<NB>];
         const unsigned char* v_before = vzero;
         if (active) {
@@ -347,8 +351,6 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
             if (slot < 8) {
 #pragma unroll
               for (int b = 0; b < NB; ++b) o[slot][b] = mfma16(f[slot], pf[b], o[slot][b]);
-              if (slot >= 2 && slot % 2 == 0 && (slot - 2) / 2 < NB)
-                psum[(slot - 2) / 2] = mfma16(ones, pf[(slot - 2) / 2], psum[(slot - 2) / 2]);
             } else {
               qk_step<NB>(s_out, f[slot], qf, slot - 8);
             }
@@ -362,7 +364,8 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
           for (int b = 0; b < NB; ++b) fine = fine && wt.sum[b] <= kMaxSum;
           if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
             qk_tile<NB>(kbuf + (j & (kBufs - 1)) * kTileBytes, fr, qf, s_in);
-            raise_max<NB>(s_in, m, l, psum, o, sl2);
+            mask(j, s_in);
+            raise_max<NB>(s_in, m, l, o, sl2);
 #pragma unroll
             for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, s_in, wt, m, sl2);
           }
@@ -377,21 +380,21 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
             __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
             __syncthreads();
             iteration(j, sa, sb);
-            if (++j >= j1) break;
+            if (++j >= n || apart(j)) break;
+            mask(j, sb);
             iteration(j, sb, sa);
-            if (++j >= j1) break;
+            if (++j >= n || apart(j)) break;
+            mask(j, sa);
           }
           pv_tile<NB>(v_before, fr, pf, o);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
         } else {
           for (;;) {
             __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
             __syncthreads();
             load(j + kAhead);
-            if (++j >= j1) break;
+            if (++j >= n || apart(j)) break;
             load(j + kAhead);
-            if (++j >= j1) break;
+            if (++j >= n || apart(j)) break;
           }
         }
       }
@@ -404,9 +407,9 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const int r = r0 + 16 * b + i16;
-        const float sum = quad_sum(l[b]), rounded = psum[b][0];
+        const float sum = quad_sum(l[b]);
         const bool live = m[b] > 0.5f * kNoMax && sum > 0.f;
-        const float inv = live ? 1.f / rounded : (sum != sum ? sum : 0.f);
+        const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
         const float lse = live ? m[b] * kLn2 + logf(sum) : -INFINITY;
         if (part) {
           const int rb = 16 * (NB * wave + b) + i16;
@@ -428,9 +431,16 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
           if (g == 0 && p.lse) p.lse[out] = lse;
         }
       }
-    if (last) return;
-    step = 0;
-    if (!next_walk(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
+    if (ahead) {
+      ahead = false;
+      seg = at.segment;
+      block = at.block;
+      kvh = at.kvh;
+      s = segment_at(p, seg);
+    } else if (same_walk(here, end) || !next_walk<true>(p, &s, &seg, &block, &kvh) ||
+               same_walk(end, ShareStart{seg, block, kvh, 0})) {
+      return;
+    }
     __syncthreads();  // every wave is done with the buffers
   }
 }

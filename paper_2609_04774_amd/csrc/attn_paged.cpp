@@ -41,17 +41,19 @@ int set_common(PagedParams* p, const std::string& who, int32_t Hq, int32_t Hkv, 
 }
 
 // Rows of a block: the fewest that hold the most rows of a sequence and KV head, up to
-// 64 with the kernel of few rows; else those of the other.
+// 32 with the kernel of few rows; else those of the other.
 constexpr int kChunkRows = 256;
 int block_rows(int64_t max_q, int32_t G) {
   const int64_t rows = max_q * G;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : kChunkRows;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : kChunkRows;
 }
+int shares_of(int block_rows) { return block_rows == kChunkRows ? kChunkShares : kRowsShares; }
 
-size_t starts_bytes() { return ((size_t)kShares * sizeof(ShareStart) + 255) / 256 * 256; }
+size_t starts_bytes(int shares) { return ((size_t)shares * sizeof(ShareStart) + 255) / 256 * 256; }
 
 size_t workspace_bytes_of(int64_t max_q, int32_t G) {
-  return starts_bytes() + 2 * (size_t)kShares * slot_floats(block_rows(max_q, G)) * 4;
+  const int rows = block_rows(max_q, G);
+  return starts_bytes(shares_of(rows)) + 2 * (size_t)shares_of(rows) * slot_floats(rows) * 4;
 }
 
 int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspace, size_t workspace_bytes, void* stream) {
@@ -60,10 +62,10 @@ int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspac
   if (!aligned(workspace, 256)) return fail(CP_ERR_INVALID, who + "workspace must be 256-byte aligned");
   if (workspace_bytes < need)
     return fail(CP_ERR_CAPACITY, who + "workspace needs " + std::to_string(need) + " bytes");
-  p->n_shares = kShares;
   p->block_rows = block_rows(max_q, p->G);
+  p->n_shares = shares_of(p->block_rows);
   p->starts = static_cast<ShareStart*>(workspace);
-  p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes());
+  p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares));
   const std::string name = who.substr(0, who.size() - 2);
   return p->block_rows == kChunkRows ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
 }

@@ -6,19 +6,19 @@
 // or among the first tokens):  x_j = scale q.k_j,  LSE = ln sum_j e^{x_j},
 // O = sum_j e^{x_j - LSE} v_j, in one pass with a running maximum and sum (Milakov
 // & Gimelshein 2018; Dao 2023).  Scores, statistics and O are fp32; the weights
-// are rounded to bf16 for the second product (at most half a step, 2^-9 of each)
-// and O is divided by the sum of the rounded ones; O is rounded once more as it is
-// stored.
+// are rounded to bf16 for the second product (half a step at most, 2^-8 of each), O is
+// rounded once more as it is stored.
 //
-// Bound by HBM: 512 bytes per key and KV head, each read once, for 16 to 64 rows.
-// The walks of all blocks, in steps of 128 keys, are cut into kShares equal parts,
-// one per workgroup and compute unit, wherever the cut falls (the lengths are
+// Bound by HBM: 512 bytes per key and KV head, each read once, for 16 or 32 rows.
+// The walks of all blocks, in steps of 128 keys, are cut into equal parts,
+// one per workgroup (two on each compute unit), wherever the cut falls (the lengths are
 // read from the device, so that a captured launch follows them): no unit waits
 // for another's longer sequence.  A part that ends inside a walk leaves a partial
 // result, and share_merge_kernel combines a walk's.  Each of a workgroup's four
-// waves takes every fourth tile of 32 keys into its own LDS (two tiles of K and of
-// V, loaded directly, the next ones in flight while one is used), so the waves
-// meet only at the end of a walk.
+// waves takes every fourth tile of 32 keys into its own LDS (K and V, loaded
+// directly, the next tile's K as soon as this one's is in registers), so the waves
+// meet only at the end of a walk; the eight waves of a compute unit keep about 128
+// KB in flight.
 #include <hip/hip_runtime.h>
 
 #include "attn_tile.h"
@@ -30,7 +30,8 @@ namespace {
 using namespace tile;
 
 constexpr int kWaves = kRowsThreads / 64;
-constexpr int kWaveBytes = 4 * kTileBytes;  // two K tiles, two V tiles
+constexpr int kWaveBytes = 2 * kTileBytes;  // a tile of K and one of V
+constexpr int kSetup = 1;                   // of a walk, in steps
 constexpr int kLoads = kTileBytes / 1024;   // direct-to-LDS loads of a tile and tensor, 1 KB each
 
 // One tile's loads of K (tensor 0) or V: 1 KB each, four keys of 256 bytes.  `off`
@@ -56,13 +57,13 @@ __device__ __forceinline__ void load_tile(const PagedParams& p, const Walk& w, i
 }
 
 template <int NB>
-__global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams p) {
+__global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams p) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * kWaveBytes];
-  __shared__ float stat[3][kWaves][16 * NB];  // per wave and row: maximum, sum, sum of the rounded weights
+  __shared__ float stat[2][kWaves][16 * NB];  // per wave and row: maximum, sum
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
-  const Share share = find_share<kRowsThreads, kWaves, 1>(p, blockIdx.x);
+  const Share share = find_share<kRowsThreads, kWaves, kSetup, 1, false>(p, blockIdx.x);
   if (tid == 0) p.starts[blockIdx.x] = share.at;
   if (same(share.at, share.end)) return;
 
@@ -74,9 +75,6 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
     const int key = 4 * q + g;
     off[q] = (uint32_t)(key * p.kv_stride) + ((i16 ^ swizzle(key)) << 4);
   }
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
 
   int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
   int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
@@ -101,13 +99,12 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
 #pragma unroll
       for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
     }
-    f32x4 o[8][NB], psum[NB];
+    f32x4 o[8][NB];
     float m[NB], l[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
-      psum[b] = f32x4{};
       m[b] = kNoMax;
       l[b] = 0.f;
     }
@@ -122,27 +119,26 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       const int jj = j + (lane >> 1);
       if (jj < n_mine) ids = page_of(p, s, tile_at(jj) + (lane & 1) * kBlockTokens);
     };
-    auto load = [&](int j, int buf, int tensor) {
-      load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + (2 * tensor + buf) * kTileBytes, tensor);
+    auto load = [&](int j, int tensor) {
+      load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + tensor * kTileBytes, tensor);
     };
-    // Tiles past the last load it again, into buffers that nobody reads: every
-    // iteration has the same number of loads in flight.
     int ids_of = 0;
     if (n_mine > 0) {
       fetch_ids(0);
-#pragma unroll 1
-      for (int x = 0; x < 4; ++x) load((x >> 1) < n_mine ? (x >> 1) : n_mine - 1, x >> 1, x & 1);
+      load(0, 0);
+      load(0, 1);
     }
+    const unsigned char* kt = mine;
+    const unsigned char* vt = mine + kTileBytes;
     for (int j = 0; j < n_mine; ++j) {
       const int t0 = tile_at(j);
-      const unsigned char* kt = mine + (j & 1) * kTileBytes;
-      const unsigned char* vt = kt + 2 * kTileBytes;
-      const int jn = j + 2 < n_mine ? j + 2 : n_mine - 1;
+      // Past the last tile it is loaded again, so that the waits can count; nobody reads it.
+      const int jn = j + 1 < n_mine ? j + 1 : j;
       if ((jn & ~31) != ids_of) {
         ids_of = jn & ~31;
         fetch_ids(ids_of);
       }
-      __builtin_amdgcn_s_waitcnt(wait_vm(3 * kLoads));  // K of tile j is in LDS
+      __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // K of tile j is in LDS
       asm volatile("" ::: "memory");
       f32x4 sc[NB][2];
       {
@@ -163,7 +159,7 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       // The K fragments are in registers (the products used them): the buffer is free.
       __builtin_amdgcn_s_waitcnt(0xC07F);
       asm volatile("" ::: "memory");
-      load(jn, j & 1, 0);
+      load(jn, 0);
 
       const bool open = open_tile(p, w, t0);
       bf16x8 pf[NB];
@@ -184,13 +180,10 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
           pf[b][r] = (__bf16)x;
         }
         l[b] = l[b] * alpha + sum;
-        psum[b] *= alpha;
 #pragma unroll
         for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
       }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) psum[b] = mfma16(ones, pf[b], psum[b]);
-      __builtin_amdgcn_s_waitcnt(wait_vm(3 * kLoads));  // V of tile j
+      __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // V of tile j
       asm volatile("" ::: "memory");
       // Keys hidden from every row are zeros; hidden from some, they may be anything.
       auto frag = [&](int db) { return v_frag(vt, lane, db); };
@@ -206,7 +199,7 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);
       asm volatile("" ::: "memory");
-      load(jn, j & 1, 1);
+      load(jn, 1);
     }
     __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no load may still be writing LDS
     asm volatile("" ::: "memory");
@@ -220,7 +213,6 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       if (g == 0) {
         stat[0][wave][r] = m[b];
         stat[1][wave][r] = sum;
-        stat[2][wave][r] = psum[b][0];
       }
 #pragma unroll
       for (int db = 0; db < 8; ++db)
@@ -234,19 +226,18 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
       float top = kNoMax;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
-      float sum = 0.f, rounded = 0.f;
+      float sum = 0.f;
       f32x4 a0 = {}, a1 = {};
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
         const float wk = __builtin_amdgcn_exp2f(stat[0][k][r] - top);
         sum += wk * stat[1][k][r];
-        rounded += wk * stat[2][k][r];
         const unsigned char* row = smem + k * kWaveBytes + r * (kHeadDim * 4);
         a0 += wk * *reinterpret_cast<const f32x4*>(row + ((c ^ (r & 15)) << 4));
         a1 += wk * *reinterpret_cast<const f32x4*>(row + (((c + 1) ^ (r & 15)) << 4));
       }
       const bool live = top > 0.5f * kNoMax && sum > 0.f;  // false for a NaN too
-      const float inv = live ? 1.f / rounded : (sum != sum ? sum : 0.f);
+      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
       const float lse = live ? top * kLn2 + logf(sum) : -INFINITY;
       a0 *= inv;
       a1 *= inv;
@@ -270,7 +261,7 @@ __global__ __launch_bounds__(kRowsThreads, 1) void attn_rows_kernel(PagedParams 
     }
     if (last) return;
     step = 0;
-    if (!next_walk(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
+    if (!next_walk<false>(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
     __syncthreads();  // the LDS is free for the next walk's tiles
   }
 }
@@ -287,10 +278,8 @@ int launch_attn_rows(const PagedParams& p, void* stream, const char* who) {
   hipStream_t st = (hipStream_t)stream;
   if (p.block_rows == 16)
     hipLaunchKernelGGL(attn_rows_kernel<1>, grid, block, 0, st, p);
-  else if (p.block_rows == 32)
-    hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);
   else
-    hipLaunchKernelGGL(attn_rows_kernel<4>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);
   const int rc = launched(who);
   return rc == CP_OK ? launch_attn_merge(p, stream, who) : rc;
 }

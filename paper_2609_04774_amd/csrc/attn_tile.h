@@ -131,10 +131,11 @@ __device__ __forceinline__ void open_tiles(const PagedParams& p, const Walk& w, 
 }
 
 // ---------------------------------------------------------------------------
-// Shares.  The walks of all blocks of rows -- in the order segment, block, KV head
-// (the heads of a block follow one another: neighbouring workgroups read the same
-// pages) -- are counted in steps of kTiles tiles and cut into equal shares, one per
-// workgroup.
+// Shares.  The walks of all blocks of rows are counted in steps of kTiles tiles and
+// cut into equal shares, one per workgroup.  Their order is segment, block, KV head
+// (neighbouring workgroups read the same pages: what HBM serves best) or, with
+// kHeadsOuter, KV head, segment, block (neighbouring workgroups, on one XCD, share
+// their keys in its L2).
 
 __device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
   return (int)(((int64_t)n * p.G + p.block_rows - 1) / p.block_rows);
@@ -158,29 +159,47 @@ __device__ __forceinline__ bool same_walk(const ShareStart& a, const ShareStart&
 }
 __device__ __forceinline__ bool same(const ShareStart& a, const ShareStart& b) { return same_walk(a, b) && a.step == b.step; }
 
+__device__ __forceinline__ ShareStart uniform(const ShareStart& x) {
+  return ShareStart{__builtin_amdgcn_readfirstlane(x.segment), __builtin_amdgcn_readfirstlane(x.block),
+                    __builtin_amdgcn_readfirstlane(x.kvh), __builtin_amdgcn_readfirstlane(x.step)};
+}
+
 // The walk after this one; false behind the last.
+template <bool kHeadsOuter>
 __device__ __forceinline__ bool next_walk(const PagedParams& p, Segment* s, int* seg, int* block, int* kvh) {
-  if (++*kvh < p.Hkv) return true;
-  *kvh = 0;
+  if (!kHeadsOuter) {
+    if (++*kvh < p.Hkv) return true;
+    *kvh = 0;
+  }
   ++*block;
   while (*block >= blocks_of(p, s->n)) {
     *block = 0;
-    if (++*seg >= p.n_segments) return false;
+    if (++*seg >= p.n_segments) {
+      if (!kHeadsOuter || ++*kvh >= p.Hkv) return false;
+      *seg = 0;
+    }
     *s = segment_at(p, *seg);
   }
   return true;
 }
 
-// A share is [at, end); behind the last walk is segment n_segments.  Each is a step
-// of a walk, or the start of one: a cut less than kSnap steps from a walk's start or
-// end moves there (a shorter part costs more than it evens out).
+// 64-bit division costs hundreds of instructions; nearly always 32 bits hold it.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((uint64_t)a | (uint64_t)b) >> 32 == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+  return a / b;
+}
+
+// A share is [at, end); behind the last walk is segment n_segments.  A walk counts as
+// its steps and kSetup more (its rows fetched, the first tiles waited for, the rows
+// stored).  A cut within those, or less than kSnap steps from the walk's start or end,
+// moves there: a shorter part costs more than it evens out.
 struct Share {
   ShareStart at, end;
 };
 
 // Every thread counts the steps of its run of segments, and a scan finds the walk of
 // each of the share's two ends.
-template <int kThreads, int kTiles, int kSnap>
+template <int kThreads, int kTiles, int kSetup, int kSnap, bool kHeadsOuter>
 __device__ Share find_share(const PagedParams& p, int share) {
   __shared__ int64_t wave_sum[kThreads / 64];
   __shared__ ShareStart found[2];
@@ -191,7 +210,7 @@ __device__ Share find_share(const PagedParams& p, int share) {
   int64_t mine = 0;
   for (int s = s0; s < s1; ++s) {
     const Segment x = segment_at(p, s);
-    for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) mine += steps_of<kTiles>(block_walk(p, x, b));
+    for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) mine += kSetup + steps_of<kTiles>(block_walk(p, x, b));
   }
   int64_t before = mine;
 #pragma unroll
@@ -209,27 +228,32 @@ __device__ Share find_share(const PagedParams& p, int share) {
     total += wave_sum[w];
   }
   before -= mine;
+  const int64_t per_head = total;
   total *= p.Hkv;
+  const int heads = kHeadsOuter ? 1 : p.Hkv;  // that share a step's place in the order
   // With fewer steps than shares the last shares are empty.
   const int64_t n = total < p.n_shares ? total : p.n_shares;
   for (int e = 0; e < 2; ++e) {
     if (share + e >= n) continue;
-    int64_t u = total * (share + e) / n - before * p.Hkv;
-    if (u < 0 || u >= mine * p.Hkv) continue;
+    int64_t u = quotient(total * (share + e), n);
+    const int head = kHeadsOuter ? (int)quotient(u, per_head) : 0;
+    u -= head * per_head + before * heads;
+    if (u < 0 || u >= mine * heads) continue;
     for (int s = s0; s < s1 && u >= 0; ++s) {
       const Segment x = segment_at(p, s);
       for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) {
-        const int steps = steps_of<kTiles>(block_walk(p, x, b));
-        if (u >= (int64_t)steps * p.Hkv) {
-          u -= (int64_t)steps * p.Hkv;
+        const int steps = kSetup + steps_of<kTiles>(block_walk(p, x, b));
+        if (u >= (int64_t)steps * heads) {
+          u -= (int64_t)steps * heads;
           continue;
         }
-        int seg = s, block = b, kvh = (int)(u / steps), step = (int)(u % steps);
+        const int k = (int)quotient(u, steps);
+        int seg = s, block = b, kvh = head + k, step = (int)(u - (int64_t)k * steps) - kSetup;
         if (step < kSnap) step = 0;
-        if (step && steps - step < kSnap) {
+        if (step && steps - kSetup - step < kSnap) {
           Segment y = x;
           step = 0;
-          if (!next_walk(p, &y, &seg, &block, &kvh)) seg = p.n_segments, block = kvh = 0;
+          if (!next_walk<kHeadsOuter>(p, &y, &seg, &block, &kvh)) seg = p.n_segments, block = kvh = 0;
         }
         found[e] = ShareStart{seg, block, kvh, step};
         u = -1;
@@ -332,18 +356,24 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 // Scores of keys that the row at position pos does not see become -inf.
-// s[half][r] is key t0 + 16 half + 4 g + r.
+// s[half][r] is key t0 + 16 half + 4 g + r.  A key at distance pos - j is seen if that
+// is in [0, window): one comparison of unsigned numbers.
 __device__ __forceinline__ void mask_scores(const PagedParams& p, f32x4 (&s)[2], int t0, int g, int pos) {
-  const int first = t0 + 4 * g;
-  const int lo = p.window ? pos - p.window : -1;  // keys above it are in the window
+  const unsigned window = p.window ? (unsigned)p.window : 1u << 31;
+  const int away = pos - (t0 + 4 * g);
+  if (__builtin_expect(p.window && t0 < p.n_sink, 0)) {
+    const int sinks = p.n_sink - (t0 + 4 * g);
 #pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int j = first + 16 * half + r;
-      if (j > pos || (j <= lo && j >= p.n_sink)) s[half][r] = -INFINITY;
-      __builtin_amdgcn_sched_barrier(0);  // one comparison's masks at a time in scalar registers
+    for (int c = 0; c < 8; ++c) {
+      const int key = 16 * (c >> 2) + (c & 3);
+      const bool seen = ((unsigned)(away - key) < window) | ((key < sinks) & (key <= away));
+      s[c >> 2][c & 3] = seen ? s[c >> 2][c & 3] : -INFINITY;
     }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      s[c >> 2][c & 3] = (unsigned)(away - (16 * (c >> 2) + (c & 3))) < window ? s[c >> 2][c & 3] : -INFINITY;
+  }
 }
 
 // Whether a V tile (its fragments v(db)) holds an infinity or a NaN: its product with

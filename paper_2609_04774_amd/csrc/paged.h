@@ -60,7 +60,8 @@ struct ShareStart {
 
 constexpr int kRowsThreads = 256;
 constexpr int kChunkThreads = 512;
-constexpr int kShares = 256;  // one workgroup per compute unit
+constexpr int kRowsShares = 512;   // workgroups: two per compute unit
+constexpr int kChunkShares = 256;  // one
 
 __host__ __device__ constexpr size_t slot_floats(int rows) { return (size_t)rows * (kHeadDim + 1); }
 
