@@ -3,7 +3,7 @@
 // those of attn_rows.hip; what differs is what bounds it, the matrix cores.
 //
 // A workgroup of 8 waves (two per SIMD: one's vector work issues while the other's
-// products run) owns 128 NB rows of one KV head, 16 NB per wave, and walks their
+// products run) owns 256 rows of one KV head, 32 per wave, and walks their
 // keys in tiles of 32 that all waves read from LDS: every fragment of K or V that
 // is read feeds NB products.  One iteration runs O += V_{j-1}^T P_{j-1}, the
 // softmax of tile j and S_{j+1} = K_{j+1} Q^T as one sequence of 16 slots, each
@@ -23,10 +23,12 @@ namespace {
 using namespace tile;
 
 constexpr int kWaves = kChunkThreads / 64;
+constexpr int NB = 2;      // blocks of 16 rows per wave
+static_assert(16 * NB * kWaves == kChunkRows, "the rows of a workgroup");
 constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % kBufs
 constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
 constexpr int kSetup = 10;  // of a walk, in tiles
-constexpr int kSnap = 12;  // tiles: a part costs its set-up, and its rows a merge
+constexpr int kSnap = 4;   // tiles: a part costs its set-up, and its rows a merge
 
 // LDS tiles by 16-byte columns: column c of a half holds chunk c of its 16 keys, key
 // k at slot k ^ 8 (c % 2).  The K reads (16 keys of a column) and the transposed V
@@ -67,10 +69,8 @@ __device__ __forceinline__ void pin(const T& x) {  // computed before this point
   asm volatile("" ::"v"(x));
 }
 
-template <int NB>
 using Scores = f32x4[NB][2];  // [block][half]
 
-template <int NB>
 struct Weights {
   float sum[NB];     // fp32 sums of this lane's weights
   bf16x2 pair[NB][4];
@@ -80,8 +80,7 @@ constexpr float kMaxSum = 65536.f;  // of a lane's 8 weights of a tile; beyond i
 
 // One unit of a tile's softmax (of 12 NB, about equal): two exponentials of a pair
 // of scores, or the pair's rounding and sum.
-template <int NB>
-__device__ __forceinline__ void softmax_unit(int u, Scores<NB>& s, Weights<NB>& w, const float (&m)[NB], float sl2) {
+__device__ __forceinline__ void softmax_unit(int u, Scores& s, Weights& w, const float (&m)[NB], float sl2) {
   const int b = u / 12, t = u % 12 / 3, kind = u % 3;  // block, pair
 
 
@@ -98,24 +97,21 @@ __device__ __forceinline__ void softmax_unit(int u, Scores<NB>& s, Weights<NB>& 
   }
 }
 
-template <int NB>
-__device__ __forceinline__ void qk_step(Scores<NB>& s, const bf16x8& k, const bf16x8 (&qf)[NB][4], int q) {
+__device__ __forceinline__ void qk_step(Scores& s, const bf16x8& k, const bf16x8 (&qf)[NB][4], int q) {
 #pragma unroll
   for (int b = 0; b < NB; ++b)
     s[b][q & 1] = mfma16(k, qf[b][q >> 1], (q >> 1) == 0 ? f32x4{} : s[b][q & 1]);
 }
 
-template <int NB>
 __device__ __forceinline__ void qk_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&qf)[NB][4],
-                                        Scores<NB>& s) {
+                                        Scores& s) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) qk_step<NB>(s, load_k(buf, f, q), qf, q);
+  for (int q = 0; q < 8; ++q) qk_step(s, load_k(buf, f, q), qf, q);
 }
 
 // Raises the running maxima to a tile's own where that is higher; O and the sums
 // follow.
-template <int NB>
-__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
+__device__ __forceinline__ void raise_max(const Scores& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     float top = s[b][0][0];
@@ -131,8 +127,7 @@ __device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], f
 }
 
 // The weights become the operand of the second product.
-template <int NB>
-__device__ __forceinline__ void finish(const Weights<NB>& w, float (&l)[NB], bf16x8 (&pf)[NB]) {
+__device__ __forceinline__ void finish(const Weights& w, float (&l)[NB], bf16x8 (&pf)[NB]) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     l[b] += w.sum[b];
@@ -142,7 +137,6 @@ __device__ __forceinline__ void finish(const Weights<NB>& w, float (&l)[NB], bf1
   }
 }
 
-template <int NB>
 __device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&pf)[NB],
                                         f32x4 (&o)[8][NB]) {
 #pragma unroll
@@ -156,7 +150,6 @@ __device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragment
 // The order of the units over an iteration: the exponentials of all blocks but the
 // last first, and the roundings from slot 8 on, when the products with the tile
 // before have freed their operand's registers.
-template <int NB>
 struct Order {
   int unit[12 * NB];
   constexpr Order() : unit{} {
@@ -174,13 +167,10 @@ struct Order {
       for (int k = t < te ? 2 : 0; k < 3; ++k) unit[n++] = last + 3 * t + k;
   }
 };
-template <int NB>
-constexpr Order<NB> kOrder{};
+constexpr Order kOrder{};
 
-template <int NB>
-constexpr int kLookahead = NB == 2 ? 3 : 2;  // slots a fragment is read ahead of its products
+constexpr int kLookahead = 3;  // slots a fragment is read ahead of its products
 
-template <int NB>
 __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParams p) {
   // The buffers of K, of V, and a V tile of zeros.
   __shared__ __attribute__((aligned(1024))) unsigned char smem[(2 * kBufs + 1) * kTileBytes];
@@ -214,33 +204,135 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   // place of walks over the same keys, so pass over the keys together.
   const ShareStart at = uniform(share.at), end = uniform(share.end);
   bool ahead = end.step > 0 && !same_walk(at, end);
-  int seg = ahead ? end.segment : at.segment, block = ahead ? end.block : at.block, kvh = ahead ? end.kvh : at.kvh;
-  Segment s = segment_at(p, seg);
-  for (;;) {
-    const Walk w = block_walk(p, s, block);
-    const int n_steps = steps_of<1>(w);
-    const ShareStart here = {seg, block, kvh, 0};
-    const int step = same_walk(here, at) ? at.step : 0;
-    const int stop = same_walk(here, end) ? end.step : n_steps;
-    const int n = w.n ? stop - step : 0;  // tiles of this part
-    const int rows = s.n * p.G, r0 = block * p.block_rows + 16 * NB * wave;
-    const bool active = r0 < rows && n > 0;  // a wave without rows only loads
+  int place = ahead ? end.place : at.place, kvh = ahead ? end.kvh : at.kvh;
+  Block x = block_at(p, place);
+  const Segment& s = x.s;
 
-    int pos[NB];
-    bf16x8 qf[NB][4];
+  // One part of a walk after another.  While the rows of one are stored, the queries
+  // and the first tiles of the next are on their way.
+  struct Rows {
+    int64_t o_row;
+    int rows, r0, kvh;  // of the segment and KV head; the wave's first
+    float* slot;        // of a part of a walk, or null
+  };
+  Rows out = {0, 0, 0, 0, nullptr};
+  Walk w;
+  int step = 0, n = 0;  // the part's first tile, and its tiles
+  int open0 = 0, open1 = 0;  // tiles of the walk that every row of the block sees whole
+  int ids = -1, ids_of = -64;  // pages of this wave's half of 64 tiles, one per lane
+  int pos[NB];
+  bf16x8 qf[NB][4];
+  f32x4 o[8][NB];
+  float m[NB], l[NB];
+  bf16x8 pf[NB];
+
+  // Tile j of the part into buffer j % kBufs; past the last it is loaded again, into
+  // a buffer nobody reads, so that the waits can count.
+  auto load = [&](int j) {
+    const uint32_t dst = load_dst + (j & (kBufs - 1)) * kTileBytes;
+    const int jj = j < n ? j : n - 1;
+    const int t0 = tile_begin(w, step + jj);
+    const int hp = t0 + load_half * kBlockTokens;
+    if (__builtin_expect((jj & ~63) != ids_of, 0)) {
+      ids_of = jj & ~63;
+      ids = -1;
+      if (ids_of + lane < n) ids = page_of(p, s, tile_begin(w, step + ids_of + lane) + load_half * kBlockTokens);
+    }
+    const HalfSource h = half_source(p, __builtin_amdgcn_readlane(ids, jj & 63), hp, kvh);
+    const unsigned char* kb = (h.paged ? p.k_cache : p.k_new) + h.offset;
+    const unsigned char* vb = (h.paged ? p.v_cache : p.v_new) + h.offset;
+    if (__builtin_expect(whole_tile(w, t0) && !h.none, 1)) {
+      load_lds(kb, load_off, dst);
+      load_lds(vb, load_off, dst + kBufs * kTileBytes);
+    } else {
+      const bool read = !h.none && walked(w, hp + load_key);
+      const unsigned char* zeros = g_zeros + load_chunk * 16;
+      load_lds_from(read ? kb + load_off : zeros, dst);
+      load_lds_from(read ? vb + load_off : zeros, dst + kBufs * kTileBytes);
+    }
+  };
+  auto closed = [&](int j) { return (step + j < open0) | (step + j >= open1); };
+  auto mask = [&](int j, Scores& sc) {
+    if (__builtin_expect(!closed(j), 1)) return;
+    const int t0 = tile_begin(w, step + j);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mask_scores(p, sc[b], t0, g, pos[b]);
+  };
+  // A tile with keys that some row does not see, and an infinity or a NaN in V (a
+  // weight of 0 times it would be a NaN): taken by itself.  Every wave looks at the
+  // same values.
+  auto apart = [&](int j) {
+    if (__builtin_expect(!closed(j), 1)) return false;
+    const unsigned char* v = vbuf + (j & (kBufs - 1)) * kTileBytes;
+    return not_finite([&](int db) { return load_v(v, fr, db); });
+  };
+  auto store = [&]() {
+    if (out.r0 >= out.rows) return;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      int r = r0 + 16 * b + i16;
-      r = r < rows ? r : rows - 1;
-      const int at = (int)((unsigned)r / (unsigned)p.G), h = r - at * p.G;
-      pos[b] = s.pos0 + at;
-      const uint16_t* q = p.q + (s.q_row + at) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+      const int r = out.r0 + 16 * b + i16;
+      const float sum = quad_sum(l[b]);
+      const bool live = m[b] > 0.5f * kNoMax && sum > 0.f;
+      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
+      const float lse = live ? m[b] * kLn2 + logf(sum) : -INFINITY;
+      if (out.slot) {
+        const int rb = 16 * (NB * wave + b) + i16;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
+        for (int db = 0; db < 8; ++db)
+          *reinterpret_cast<f32x4*>(out.slot + rb * kHeadDim + 16 * db + 4 * g) = o[db][b] * inv;
+        // A NaN among the scores is an LSE of NaN here: the merge tells it from a part without keys.
+        if (g == 0) out.slot[p.block_rows * kHeadDim + rb] = sum != sum ? sum : lse;
+      } else if (r < out.rows) {
+        const int q = (int)((unsigned)r / (unsigned)p.G);
+        const int64_t row = (out.o_row + q) * p.Hq + out.kvh * p.G + (r - q * p.G);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+          typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[db][b][e] * inv);
+          *reinterpret_cast<bf16x4*>(p.o + row * kHeadDim + 16 * db + 4 * g) = v;
+        }
+        if (g == 0 && p.lse) p.lse[row] = lse;
+      }
     }
-    f32x4 o[8][NB];
-    float m[NB], l[NB];
-    bf16x8 pf[NB];
+  };
+
+  for (bool first = true, more = true;; first = false) {
+    const ShareStart here = {place, kvh, 0, 0};
+    Rows now = out;
+    if (more) {
+      w = block_walk(p, s, x.block);
+      const int n_steps = steps_of<1>(w);
+      step = same_walk(here, at) ? at.step : 0;
+      const int stop = same_walk(here, end) ? end.step : n_steps;
+      n = w.n ? stop - step : 0;
+      now.o_row = s.o_row;
+      now.rows = s.n * p.G;
+      now.r0 = x.block * p.block_rows + 16 * NB * wave;
+      now.kvh = kvh;
+      now.slot = step > 0 || stop < n_steps
+                     ? p.slots + (2 * (size_t)number + (step > 0 ? 0 : 1)) * slot_floats(p.block_rows)
+                     : nullptr;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        int r = now.r0 + 16 * b + i16;
+        r = r < now.rows ? r : now.rows - 1;
+        const int q = (int)((unsigned)r / (unsigned)p.G), h = r - q * p.G;
+        pos[b] = s.pos0 + q;
+        const uint16_t* from = p.q + (s.q_row + q) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(from + 32 * d);
+      }
+      open_tiles(p, w, &open0, &open1);
+      ids_of = -64;
+      if (n > 0)
+        for (int j = 0; j < kAhead; ++j) load(j);
+    }
+    if (!first) store();
+    if (!more) return;
+    out = now;
+    const bool active = out.r0 < out.rows;  // a wave without rows only loads
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -250,52 +342,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
       l[b] = 0.f;
     }
 
-    int ids = -1, ids_of = -64;  // pages of this wave's half of 64 tiles, one per lane
-    // Tile j of the part into buffer j % kBufs; past the last it is loaded again, into
-    // a buffer nobody reads, so that the waits can count.
-    auto load = [&](int j) {
-      const uint32_t dst = load_dst + (j & (kBufs - 1)) * kTileBytes;
-      const int jj = j < n ? j : n - 1;
-      const int t0 = tile_begin(w, step + jj);
-      const int hp = t0 + load_half * kBlockTokens;
-      if (__builtin_expect((jj & ~63) != ids_of, 0)) {
-        ids_of = jj & ~63;
-        ids = -1;
-        if (ids_of + lane < n) ids = page_of(p, s, tile_begin(w, step + ids_of + lane) + load_half * kBlockTokens);
-      }
-      const HalfSource h = half_source(p, __builtin_amdgcn_readlane(ids, jj & 63), hp, kvh);
-      const unsigned char* kb = (h.paged ? p.k_cache : p.k_new) + h.offset;
-      const unsigned char* vb = (h.paged ? p.v_cache : p.v_new) + h.offset;
-      if (__builtin_expect(whole_tile(w, t0) && !h.none, 1)) {
-        load_lds(kb, load_off, dst);
-        load_lds(vb, load_off, dst + kBufs * kTileBytes);
-      } else {
-        const bool read = !h.none && walked(w, hp + load_key);
-        const unsigned char* zeros = g_zeros + load_chunk * 16;
-        load_lds_from(read ? kb + load_off : zeros, dst);
-        load_lds_from(read ? vb + load_off : zeros, dst + kBufs * kTileBytes);
-      }
-    };
     if (n > 0) {
-      __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the query fragments
-      for (int j = 0; j < kAhead; ++j) load(j);
-      int open0, open1;  // tiles of the walk that every row of the block sees whole
-      open_tiles(p, w, &open0, &open1);
-      auto closed = [&](int j) { return (step + j < open0) | (step + j >= open1); };
-      auto mask = [&](int j, Scores<NB>& sc) {
-        if (__builtin_expect(!closed(j), 1)) return;
-        const int t0 = tile_begin(w, step + j);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) mask_scores(p, sc[b], t0, g, pos[b]);
-      };
-      // A tile with keys that some row does not see, and an infinity or a NaN in V (a
-      // weight of 0 times it would be a NaN): taken by itself.  Every wave looks at the
-      // same values.
-      auto apart = [&](int j) {
-        if (__builtin_expect(!closed(j), 1)) return false;
-        const unsigned char* v = vbuf + (j & (kBufs - 1)) * kTileBytes;
-        return not_finite([&](int db) { return load_v(v, fr, db); });
-      };
       int j = 0;
 #pragma unroll 1
       while (j < n) {
@@ -304,19 +351,19 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         __syncthreads();
         const unsigned char* k_now = kbuf + (j & (kBufs - 1)) * kTileBytes;
         const unsigned char* v_now = vbuf + (j & (kBufs - 1)) * kTileBytes;
-        Scores<NB> sa, sb;
-        Weights<NB> wt;
+        Scores sa, sb;
+        Weights wt;
         if (active) {
-          qk_tile<NB>(k_now, fr, qf, sa);
+          qk_tile(k_now, fr, qf, sa);
           mask(j, sa);
-          raise_max<NB>(sa, m, l, o, sl2);
+          raise_max(sa, m, l, o, sl2);
         }
         if (__builtin_expect(apart(j), 0)) {
           load(j + kAhead);
           if (active) {
 #pragma unroll
-            for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, sa, wt, m, sl2);
-            finish<NB>(wt, l, pf);
+            for (int u = 0; u < 12 * NB; ++u) softmax_unit(u, sa, wt, m, sl2);
+            finish(wt, l, pf);
             pv_not_finite<NB>([&](int db) { return load_v(v_now, fr, db); }, pf, o);
           }
           ++j;
@@ -324,24 +371,24 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         }
         // The tiles up to the next such one, pipelined.  No tile before the first: its V
         // is zeros.
-        bf16x8 pre[kLookahead<NB>];
+        bf16x8 pre[kLookahead];
         const unsigned char* v_before = vzero;
         if (active) {
 #pragma unroll
           for (int b = 0; b < NB; ++b) pf[b] = bf16x8{};
 #pragma unroll
-          for (int x = 0; x < kLookahead<NB>; ++x) pre[x] = load_v(vzero, fr, x);
+          for (int x = 0; x < kLookahead; ++x) pre[x] = load_v(vzero, fr, x);
         }
-        auto iteration = [&](int j, Scores<NB>& s_in, Scores<NB>& s_out) {
+        auto iteration = [&](int j, Scores& s_in, Scores& s_out) {
           const unsigned char* k_next = kbuf + ((j + 1) & (kBufs - 1)) * kTileBytes;
           const unsigned char* v_this = vbuf + (j & (kBufs - 1)) * kTileBytes;
           load(j + kAhead);
           bf16x8 f[16];
 #pragma unroll
-          for (int x = 0; x < kLookahead<NB>; ++x) f[x] = pre[x];
+          for (int x = 0; x < kLookahead; ++x) f[x] = pre[x];
 #pragma unroll
           for (int slot = 0; slot < 16; ++slot) {
-            const int x = slot + kLookahead<NB>;
+            const int x = slot + kLookahead;
             if (x < 8)
               f[x] = load_v(v_before, fr, x);
             else if (x < 16)
@@ -352,24 +399,24 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
 #pragma unroll
               for (int b = 0; b < NB; ++b) o[slot][b] = mfma16(f[slot], pf[b], o[slot][b]);
             } else {
-              qk_step<NB>(s_out, f[slot], qf, slot - 8);
+              qk_step(s_out, f[slot], qf, slot - 8);
             }
 #pragma unroll
             for (int u = slot * 12 * NB / 16; u < (slot + 1) * 12 * NB / 16; ++u)
-              softmax_unit<NB>(kOrder<NB>.unit[u], s_in, wt, m, sl2);
+              softmax_unit(kOrder.unit[u], s_in, wt, m, sl2);
             __builtin_amdgcn_sched_barrier(0);
           }
           bool fine = true;
 #pragma unroll
           for (int b = 0; b < NB; ++b) fine = fine && wt.sum[b] <= kMaxSum;
           if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
-            qk_tile<NB>(kbuf + (j & (kBufs - 1)) * kTileBytes, fr, qf, s_in);
+            qk_tile(kbuf + (j & (kBufs - 1)) * kTileBytes, fr, qf, s_in);
             mask(j, s_in);
-            raise_max<NB>(s_in, m, l, o, sl2);
+            raise_max(s_in, m, l, o, sl2);
 #pragma unroll
-            for (int u = 0; u < 12 * NB; ++u) softmax_unit<NB>(u, s_in, wt, m, sl2);
+            for (int u = 0; u < 12 * NB; ++u) softmax_unit(u, s_in, wt, m, sl2);
           }
-          finish<NB>(wt, l, pf);
+          finish(wt, l, pf);
           v_before = v_this;
         };
         // In pairs behind one barrier (the first pair's is above): at a pair's start
@@ -386,7 +433,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
             if (++j >= n || apart(j)) break;
             mask(j, sa);
           }
-          pv_tile<NB>(v_before, fr, pf, o);
+          pv_tile(v_before, fr, pf, o);
         } else {
           for (;;) {
             __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
@@ -401,45 +448,14 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
       __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no load may still be writing LDS
     }
 
-    const bool part = step > 0 || stop < n_steps;
-    float* slot = p.slots + (2 * (size_t)number + (step > 0 ? 0 : 1)) * slot_floats(p.block_rows);
-    if (r0 < rows)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int r = r0 + 16 * b + i16;
-        const float sum = quad_sum(l[b]);
-        const bool live = m[b] > 0.5f * kNoMax && sum > 0.f;
-        const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
-        const float lse = live ? m[b] * kLn2 + logf(sum) : -INFINITY;
-        if (part) {
-          const int rb = 16 * (NB * wave + b) + i16;
-#pragma unroll
-          for (int db = 0; db < 8; ++db)
-            *reinterpret_cast<f32x4*>(slot + rb * kHeadDim + 16 * db + 4 * g) = o[db][b] * inv;
-          if (g == 0) slot[p.block_rows * kHeadDim + rb] = sum != sum ? sum : lse;
-        } else if (r < rows) {
-          const int at = (int)((unsigned)r / (unsigned)p.G);
-          const int64_t out = (s.o_row + at) * p.Hq + kvh * p.G + (r - at * p.G);
-#pragma unroll
-          for (int db = 0; db < 8; ++db) {
-            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-            bf16x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[db][b][e] * inv);
-            *reinterpret_cast<bf16x4*>(p.o + out * kHeadDim + 16 * db + 4 * g) = v;
-          }
-          if (g == 0 && p.lse) p.lse[out] = lse;
-        }
-      }
     if (ahead) {
       ahead = false;
-      seg = at.segment;
-      block = at.block;
+      place = at.place;
       kvh = at.kvh;
-      s = segment_at(p, seg);
-    } else if (same_walk(here, end) || !next_walk<true>(p, &s, &seg, &block, &kvh) ||
-               same_walk(end, ShareStart{seg, block, kvh, 0})) {
-      return;
+      x = block_at(p, place);
+    } else {
+      more = !same_walk(here, end) && next_walk<true>(p, &x, &place, &kvh) &&
+             !same_walk(end, ShareStart{place, kvh, 0, 0});
     }
     __syncthreads();  // every wave is done with the buffers
   }
@@ -449,10 +465,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
 
 int launch_attn_chunk(const PagedParams& p, void* stream, const char* who) {
   const dim3 grid((unsigned)p.n_shares), block(kChunkThreads);
-  if (p.block_rows == 16 * kWaves * 2)
-    hipLaunchKernelGGL(attn_chunk_kernel<2>, grid, block, 0, (hipStream_t)stream, p);
-  else
-    hipLaunchKernelGGL(attn_chunk_kernel<3>, grid, block, 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(attn_chunk_kernel, grid, block, 0, (hipStream_t)stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));
   return launch_attn_merge(p, stream, who);

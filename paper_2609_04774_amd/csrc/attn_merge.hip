@@ -28,9 +28,10 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
   const ShareStart at = p.starts[share];
   ShareStart next = share + 1 + lane < p.n_shares ? p.starts[share + 1 + lane] : none;
   if (at.step == 0 || (same_walk(before, at) && before.step > 0)) return;
-  const Segment s = segment_at(p, at.segment);
+  const Block x = block_at(p, at.place);
+  const Segment& s = x.s;
   const int r0 = kRows * (4 * blockIdx.y + (threadIdx.x >> 6));  // of the block
-  const int rows = s.n * p.G - at.block * p.block_rows;
+  const int rows = s.n * p.G - x.block * p.block_rows;
   if (r0 >= rows) return;
   int n = 2;  // parts
   for (;;) {
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
     for (int k = 1; k < 64; k *= 2) sum[i] += __shfl_xor(sum[i], k);
     if (r0 + i >= rows) continue;
     const float inv = top[i] == -INFINITY ? 0.f : 1.f / sum[i];
-    const int row = at.block * p.block_rows + r0 + i;
+    const int row = x.block * p.block_rows + r0 + i;
     const int q = (int)((unsigned)row / (unsigned)p.G);
     const int64_t out = (s.o_row + q) * p.Hq + at.kvh * p.G + (row - q * p.G);
     reinterpret_cast<bf16x2*>(p.o + out * kHeadDim)[lane] = bf16x2{(__bf16)(acc[i].x * inv), (__bf16)(acc[i].y * inv)};

@@ -42,7 +42,6 @@ int set_common(PagedParams* p, const std::string& who, int32_t Hq, int32_t Hkv, 
 
 // Rows of a block: the fewest that hold the most rows of a sequence and KV head, up to
 // 32 with the kernel of few rows; else those of the other.
-constexpr int kChunkRows = 256;
 int block_rows(int64_t max_q, int32_t G) {
   const int64_t rows = max_q * G;
   return rows <= 16 ? 16 : rows <= 32 ? 32 : kChunkRows;
@@ -64,6 +63,14 @@ int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspac
     return fail(CP_ERR_CAPACITY, who + "workspace needs " + std::to_string(need) + " bytes");
   p->block_rows = block_rows(max_q, p->G);
   p->n_shares = shares_of(p->block_rows);
+  p->blocks = (int32_t)((max_q * p->G + p->block_rows - 1) / p->block_rows);
+  const int64_t places = (int64_t)p->n_segments * p->blocks;
+  if (places > INT32_MAX / 2) return fail(CP_ERR_UNSUPPORTED, who + "too many sequences of so many rows");
+  // Blocks of a share, where each has several (of those that may have rows).
+  const int64_t full = p->n_rows * p->G / p->block_rows + p->n_segments;
+  const int64_t run = (full < places ? full : places) * p->Hkv / p->n_shares;
+  p->run = p->block_rows == kChunkRows && run > 1 ? (int32_t)run : 1;
+  p->stride = (int32_t)((places + p->run - 1) / p->run);
   p->starts = static_cast<ShareStart*>(workspace);
   p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares));
   const std::string name = who.substr(0, who.size() - 2);

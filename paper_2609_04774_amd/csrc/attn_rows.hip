@@ -76,14 +76,17 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     off[q] = (uint32_t)(key * p.kv_stride) + ((i16 ^ swizzle(key)) << 4);
   }
 
-  int seg = __builtin_amdgcn_readfirstlane(share.at.segment), block = __builtin_amdgcn_readfirstlane(share.at.block);
-  int kvh = __builtin_amdgcn_readfirstlane(share.at.kvh), step = __builtin_amdgcn_readfirstlane(share.at.step);
-  Segment s = segment_at(p, seg);
+  const ShareStart end = uniform(share.end);
+  int place = __builtin_amdgcn_readfirstlane(share.at.place), kvh = __builtin_amdgcn_readfirstlane(share.at.kvh);
+  int step = __builtin_amdgcn_readfirstlane(share.at.step);
+  Block x = block_at(p, place);
   for (;;) {
+    const Segment& s = x.s;
+    const int block = x.block;
     const Walk w = block_walk(p, s, block);
     const int n_steps = steps_of<kWaves>(w);
-    const bool last = same_walk(share.end, ShareStart{seg, block, kvh, 0});
-    const int stop = last ? share.end.step : n_steps;
+    const bool last = same_walk(end, ShareStart{place, kvh, 0, 0});
+    const int stop = last ? end.step : n_steps;
     const int rows = s.n * p.G, r0 = block * p.block_rows;
 
     // Rows past the block's end repeat its last one and are not stored.
@@ -221,8 +224,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     __syncthreads();
     const bool part = step > 0 || stop < n_steps;
     float* slot = p.slots + (2 * (size_t)blockIdx.x + (step > 0 ? 0 : 1)) * slot_floats(16 * NB);
-    for (int x = tid; x < 16 * NB * 16; x += kRowsThreads) {  // 8 values of a row each
-      const int r = x >> 4, c = (x & 15) * 2;
+    for (int y = tid; y < 16 * NB * 16; y += kRowsThreads) {  // 8 values of a row each
+      const int r = y >> 4, c = (y & 15) * 2;
       float top = kNoMax;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     }
     if (last) return;
     step = 0;
-    if (!next_walk<false>(p, &s, &seg, &block, &kvh) || same(share.end, ShareStart{seg, block, kvh, 0})) return;
+    if (!next_walk<false>(p, &x, &place, &kvh) || same(end, ShareStart{place, kvh, 0, 0})) return;
     __syncthreads();  // the LDS is free for the next walk's tiles
   }
 }

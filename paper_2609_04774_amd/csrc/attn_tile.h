@@ -132,14 +132,14 @@ __device__ __forceinline__ void open_tiles(const PagedParams& p, const Walk& w, 
 
 // ---------------------------------------------------------------------------
 // Shares.  The walks of all blocks of rows are counted in steps of kTiles tiles and
-// cut into equal shares, one per workgroup.  Their order is segment, block, KV head
+// cut into equal shares, one per workgroup.  Blocks are numbered as if every segment
+// had as many as the longest may have (the others have no rows and no steps), and
+// come in an order (PagedParams::run) that gives a workgroup, of a launch of several
+// blocks each, blocks far apart: those of neighbouring workgroups then pass over the
+// same keys at the same time.  The walks of a block's KV heads follow one another
 // (neighbouring workgroups read the same pages: what HBM serves best) or, with
-// kHeadsOuter, KV head, segment, block (neighbouring workgroups, on one XCD, share
-// their keys in its L2).
-
-__device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
-  return (int)(((int64_t)n * p.G + p.block_rows - 1) / p.block_rows);
-}
+// kHeadsOuter, all blocks of a KV head do (the workgroups of an XCD share their keys in
+// its L2).
 
 __device__ __forceinline__ Walk block_walk(const PagedParams& p, const Segment& s, int block) {
   const int r0 = block * p.block_rows;
@@ -155,31 +155,50 @@ __device__ __forceinline__ int steps_of(const Walk& w) {
 }
 
 __device__ __forceinline__ bool same_walk(const ShareStart& a, const ShareStart& b) {
-  return a.segment == b.segment && a.block == b.block && a.kvh == b.kvh;
+  return a.place == b.place && a.kvh == b.kvh;
 }
 __device__ __forceinline__ bool same(const ShareStart& a, const ShareStart& b) { return same_walk(a, b) && a.step == b.step; }
-
 __device__ __forceinline__ ShareStart uniform(const ShareStart& x) {
-  return ShareStart{__builtin_amdgcn_readfirstlane(x.segment), __builtin_amdgcn_readfirstlane(x.block),
-                    __builtin_amdgcn_readfirstlane(x.kvh), __builtin_amdgcn_readfirstlane(x.step)};
+  return ShareStart{__builtin_amdgcn_readfirstlane(x.place), __builtin_amdgcn_readfirstlane(x.kvh),
+                    __builtin_amdgcn_readfirstlane(x.step), 0};
 }
 
-// The walk after this one; false behind the last.
+// Places of the launch's order: run * stride, at least a place for each block.
+__device__ __forceinline__ int places(const PagedParams& p) { return p.run * p.stride; }
+
+struct Block {
+  Segment s;
+  int block;
+  bool rows;  // it has any
+};
+
+__device__ __forceinline__ Block block_at(const PagedParams& p, int place) {
+  Block x;
+  const int i = p.run == 1 ? place : place % p.run * p.stride + place / p.run;
+  const int seg = p.blocks == 1 ? i : (int)((unsigned)i / (unsigned)p.blocks);
+  x.block = i - seg * p.blocks;
+  x.rows = false;
+  if (seg < p.n_segments) {
+    x.s = segment_at(p, seg);
+    x.rows = (int64_t)x.block * p.block_rows < (int64_t)x.s.n * p.G;
+  }
+  return x;
+}
+
+// The walk after this one, at its block; false behind the last.
 template <bool kHeadsOuter>
-__device__ __forceinline__ bool next_walk(const PagedParams& p, Segment* s, int* seg, int* block, int* kvh) {
+__device__ __forceinline__ bool next_walk(const PagedParams& p, Block* x, int* place, int* kvh) {
   if (!kHeadsOuter) {
     if (++*kvh < p.Hkv) return true;
     *kvh = 0;
   }
-  ++*block;
-  while (*block >= blocks_of(p, s->n)) {
-    *block = 0;
-    if (++*seg >= p.n_segments) {
+  do {
+    if (++*place >= places(p)) {
       if (!kHeadsOuter || ++*kvh >= p.Hkv) return false;
-      *seg = 0;
+      *place = 0;
     }
-    *s = segment_at(p, *seg);
-  }
+    *x = block_at(p, *place);
+  } while (!x->rows);
   return true;
 }
 
@@ -189,29 +208,31 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return a / b;
 }
 
-// A share is [at, end); behind the last walk is segment n_segments.  A walk counts as
-// its steps and kSetup more (its rows fetched, the first tiles waited for, the rows
+// A share is [at, end); behind the last walk is place places(p).  A walk counts as its
+// steps and kSetup more (its rows fetched, the first tiles waited for, the rows
 // stored).  A cut within those, or less than kSnap steps from the walk's start or end,
 // moves there: a shorter part costs more than it evens out.
 struct Share {
   ShareStart at, end;
 };
 
-// Every thread counts the steps of its run of segments, and a scan finds the walk of
+// Every thread counts the steps of its run of places, and a scan finds the walk of
 // each of the share's two ends.
 template <int kThreads, int kTiles, int kSetup, int kSnap, bool kHeadsOuter>
 __device__ Share find_share(const PagedParams& p, int share) {
   __shared__ int64_t wave_sum[kThreads / 64];
   __shared__ ShareStart found[2];
   const int tid = threadIdx.x;
-  const int per = (p.n_segments + kThreads - 1) / kThreads;
-  const int s0 = tid * per < p.n_segments ? tid * per : p.n_segments;
-  const int s1 = s0 + per < p.n_segments ? s0 + per : p.n_segments;
+  const int n_places = places(p);
+  const int per = (n_places + kThreads - 1) / kThreads;
+  const int i0 = tid * per < n_places ? tid * per : n_places;
+  const int i1 = i0 + per < n_places ? i0 + per : n_places;
+  auto cost_of = [&](int place) {
+    const Block x = block_at(p, place);
+    return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, x.s, x.block)) : 0;
+  };
   int64_t mine = 0;
-  for (int s = s0; s < s1; ++s) {
-    const Segment x = segment_at(p, s);
-    for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) mine += kSetup + steps_of<kTiles>(block_walk(p, x, b));
-  }
+  for (int i = i0; i < i1; ++i) mine += cost_of(i);
   int64_t before = mine;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) {
@@ -219,7 +240,7 @@ __device__ Share find_share(const PagedParams& p, int share) {
     if ((tid & 63) >= k) before += x;
   }
   if ((tid & 63) == 63) wave_sum[tid >> 6] = before;
-  if (tid < 2) found[tid] = ShareStart{p.n_segments, 0, 0, 0};
+  if (tid < 2) found[tid] = ShareStart{n_places, 0, 0, 0};
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
@@ -228,7 +249,7 @@ __device__ Share find_share(const PagedParams& p, int share) {
     total += wave_sum[w];
   }
   before -= mine;
-  const int64_t per_head = total;
+  const int64_t per_head = total > 0 ? total : 1;
   total *= p.Hkv;
   const int heads = kHeadsOuter ? 1 : p.Hkv;  // that share a step's place in the order
   // With fewer steps than shares the last shares are empty.
@@ -239,26 +260,22 @@ __device__ Share find_share(const PagedParams& p, int share) {
     const int head = kHeadsOuter ? (int)quotient(u, per_head) : 0;
     u -= head * per_head + before * heads;
     if (u < 0 || u >= mine * heads) continue;
-    for (int s = s0; s < s1 && u >= 0; ++s) {
-      const Segment x = segment_at(p, s);
-      for (int b = 0, nb = blocks_of(p, x.n); b < nb; ++b) {
-        const int steps = kSetup + steps_of<kTiles>(block_walk(p, x, b));
-        if (u >= (int64_t)steps * heads) {
-          u -= (int64_t)steps * heads;
-          continue;
-        }
-        const int k = (int)quotient(u, steps);
-        int seg = s, block = b, kvh = head + k, step = (int)(u - (int64_t)k * steps) - kSetup;
-        if (step < kSnap) step = 0;
-        if (step && steps - kSetup - step < kSnap) {
-          Segment y = x;
-          step = 0;
-          if (!next_walk<kHeadsOuter>(p, &y, &seg, &block, &kvh)) seg = p.n_segments, block = kvh = 0;
-        }
-        found[e] = ShareStart{seg, block, kvh, step};
-        u = -1;
-        break;
+    for (int i = i0; i < i1; ++i) {
+      const int cost = cost_of(i);
+      if (u >= (int64_t)cost * heads) {
+        u -= (int64_t)cost * heads;
+        continue;
       }
+      const int k = (int)quotient(u, cost);
+      int place = i, kvh = head + k, step = (int)(u - (int64_t)k * cost) - kSetup;
+      if (step < kSnap) step = 0;
+      if (step && cost - kSetup - step < kSnap) {
+        Block next;
+        step = 0;
+        if (!next_walk<kHeadsOuter>(p, &next, &place, &kvh)) place = n_places, kvh = 0;
+      }
+      found[e] = ShareStart{place, kvh, step, 0};
+      break;
     }
   }
   __syncthreads();

@@ -48,18 +48,21 @@ struct PagedParams {
   // partial results per workgroup.
   int32_t n_shares;
   int32_t block_rows;      // rows of a block (of one KV head)
+  int32_t blocks;          // of a segment, at most
+  int32_t stride, run;     // order of the blocks: place i is block (i % run) * stride + i / run
   struct ShareStart* starts;
   float* slots;
 };
 
 // Where a workgroup's share of the launch begins: a step (of tiles) of the walk of
-// one block of rows of one segment and KV head.
+// one block of rows (its place in the launch's order) and KV head.
 struct ShareStart {
-  int32_t segment, block, kvh, step;
+  int32_t place, kvh, step, reserved;
 };
 
 constexpr int kRowsThreads = 256;
 constexpr int kChunkThreads = 512;
+constexpr int kChunkRows = 256;  // rows of a block of the kernel of many rows
 constexpr int kRowsShares = 512;   // workgroups: two per compute unit
 constexpr int kChunkShares = 256;  // one
 
