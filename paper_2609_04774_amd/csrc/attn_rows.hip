@@ -80,56 +80,131 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   int place = __builtin_amdgcn_readfirstlane(share.at.place), kvh = __builtin_amdgcn_readfirstlane(share.at.kvh);
   int step = __builtin_amdgcn_readfirstlane(share.at.step);
   Block x = block_at(p, place);
-  for (;;) {
-    const Segment& s = x.s;
-    const int block = x.block;
-    const Walk w = block_walk(p, s, block);
-    const int n_steps = steps_of<kWaves>(w);
-    const bool last = same_walk(end, ShareStart{place, kvh, 0, 0});
-    const int stop = last ? end.step : n_steps;
-    const int rows = s.n * p.G, r0 = block * p.block_rows;
+  const Segment& s = x.s;
 
-    // Rows past the block's end repeat its last one and are not stored.
-    int pos[NB];
-    bf16x8 qf[NB][4];  // B of S^T = K Q^T: row i16 of block b, head dims 32 step + 8 g ..
+  // One part of a walk after another.  While the rows of one are combined and stored,
+  // the queries and the pages of the next are on their way.
+  struct Rows {
+    int64_t o_row;
+    int rows, r0, kvh;  // of the segment and KV head; the block's first
+    float* slot;        // of a part of a walk, or null
+  };
+  Rows out = {0, 0, 0, 0, nullptr};
+  Walk w;
+  int n_mine = 0;  // this wave's tiles: kWaves (step + j) + wave for j below n_mine
+  int ids = -1;    // pages of the halves of tiles 32 (j / 32) .. of this wave, one per lane
+  int pos[NB];
+  bf16x8 qf[NB][4];  // B of S^T = K Q^T: row i16 of block b, head dims 32 step + 8 g ..
+  f32x4 o[8][NB];
+  float m[NB], l[NB];
+  auto tile_at = [&](int j) { return tile_begin(w, kWaves * (step + j) + wave); };
+  auto fetch_ids = [&](int j) {
+    ids = -1;
+    const int jj = j + (lane >> 1);
+    if (jj < n_mine) ids = page_of(p, s, tile_at(jj) + (lane & 1) * kBlockTokens);
+  };
+  auto load = [&](int j, int tensor) {
+    load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + tensor * kTileBytes, tensor);
+  };
+  // The four waves' results, unnormalised, row by row through LDS: float4 c of row r at
+  // slot c ^ (r % 16) of its row.
+  auto store = [&]() {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      int r = r0 + 16 * b + i16;
-      r = r < rows ? r : rows - 1;
-      const int at = (int)((unsigned)r / (unsigned)p.G), h = r - at * p.G;
-      pos[b] = s.pos0 + at;
-      const uint16_t* q = p.q + (s.q_row + at) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+      const int r = 16 * b + i16;
+      const float sum = quad_sum(l[b]);
+      if (g == 0) {
+        stat[0][wave][r] = m[b];
+        stat[1][wave][r] = sum;
+      }
 #pragma unroll
-      for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
+      for (int db = 0; db < 8; ++db)
+        *reinterpret_cast<f32x4*>(mine + r * (kHeadDim * 4) + (((4 * db + g) ^ i16) << 4)) = o[db][b];
     }
-    f32x4 o[8][NB];
-    float m[NB], l[NB];
+    __syncthreads();
+    for (int y = tid; y < 16 * NB * 16; y += kRowsThreads) {  // 8 values of a row each
+      const int r = y >> 4, c = (y & 15) * 2;
+      float top = kNoMax;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
+      float sum = 0.f;
+      f32x4 a0 = {}, a1 = {};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float wk = __builtin_amdgcn_exp2f(stat[0][k][r] - top);
+        sum += wk * stat[1][k][r];
+        const unsigned char* row = smem + k * kWaveBytes + r * (kHeadDim * 4);
+        a0 += wk * *reinterpret_cast<const f32x4*>(row + ((c ^ (r & 15)) << 4));
+        a1 += wk * *reinterpret_cast<const f32x4*>(row + (((c + 1) ^ (r & 15)) << 4));
+      }
+      const bool live = top > 0.5f * kNoMax && sum > 0.f;  // false for a NaN too
+      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
+      const float lse = live ? top * kLn2 + logf(sum) : -INFINITY;
+      a0 *= inv;
+      a1 *= inv;
+      if (out.slot) {
+        // A NaN among the scores is an LSE of NaN here: the merge tells it from a part without keys.
+        *reinterpret_cast<f32x4*>(out.slot + r * kHeadDim + 4 * c) = a0;
+        *reinterpret_cast<f32x4*>(out.slot + r * kHeadDim + 4 * c + 4) = a1;
+        if (c == 0) out.slot[16 * NB * kHeadDim + r] = sum != sum ? sum : lse;
+      } else if (out.r0 + r < out.rows) {
+        const int at = (int)((unsigned)(out.r0 + r) / (unsigned)p.G);
+        const int64_t row = (out.o_row + at) * p.Hq + out.kvh * p.G + (out.r0 + r - at * p.G);
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = (__bf16)a0[e];
+          v[4 + e] = (__bf16)a1[e];
+        }
+        *reinterpret_cast<bf16x8*>(p.o + row * kHeadDim + 4 * c) = v;
+        if (c == 0 && p.lse) p.lse[row] = lse;
+      }
+    }
+    __syncthreads();  // the LDS is free for the next part's tiles
+  };
+
+  for (bool first = true, more = true;; first = false) {
+    Rows now = out;
+    if (more) {
+      w = block_walk(p, s, x.block);
+      const int n_steps = steps_of<kWaves>(w);
+      const int stop = same_walk(end, ShareStart{place, kvh, 0, 0}) ? end.step : n_steps;
+      now.o_row = s.o_row;
+      now.rows = s.n * p.G;
+      now.r0 = x.block * p.block_rows;
+      now.kvh = kvh;
+      now.slot = step > 0 || stop < n_steps
+                     ? p.slots + (2 * (size_t)blockIdx.x + (step > 0 ? 0 : 1)) * slot_floats(16 * NB)
+                     : nullptr;
+      // Rows past the block's end repeat its last one and are not stored.
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        int r = now.r0 + 16 * b + i16;
+        r = r < now.rows ? r : now.rows - 1;
+        const int at = (int)((unsigned)r / (unsigned)p.G), h = r - at * p.G;
+        pos[b] = s.pos0 + at;
+        const uint16_t* q = p.q + (s.q_row + at) * p.q_stride + (int64_t)(kvh * p.G + h) * kHeadDim + 8 * g;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(q + 32 * d);
+      }
+      const int t_end = w.n < kWaves * stop ? w.n : kWaves * stop;
+      n_mine = (t_end - kWaves * step - wave + kWaves - 1) / kWaves;
+      fetch_ids(0);
+    }
+    if (!first) store();
+    if (!more) return;
+    out = now;
+    int ids_of = 0;
+    if (n_mine > 0) {
+      load(0, 0);
+      load(0, 1);
+    }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
       m[b] = kNoMax;
       l[b] = 0.f;
-    }
-
-    // This wave's tiles: kWaves * j + wave for j in [step, stop), below w.n.
-    const int t_end = w.n < kWaves * stop ? w.n : kWaves * stop;
-    const int n_mine = (t_end - kWaves * step - wave + kWaves - 1) / kWaves;
-    int ids = -1;  // pages of the halves of tiles 32 (j / 32) .. of this wave, one per lane
-    auto tile_at = [&](int j) { return tile_begin(w, kWaves * (step + j) + wave); };
-    auto fetch_ids = [&](int j) {
-      ids = -1;
-      const int jj = j + (lane >> 1);
-      if (jj < n_mine) ids = page_of(p, s, tile_at(jj) + (lane & 1) * kBlockTokens);
-    };
-    auto load = [&](int j, int tensor) {
-      load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + tensor * kTileBytes, tensor);
-    };
-    int ids_of = 0;
-    if (n_mine > 0) {
-      fetch_ids(0);
-      load(0, 0);
-      load(0, 1);
     }
     const unsigned char* kt = mine;
     const unsigned char* vt = mine + kTileBytes;
@@ -207,65 +282,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     __builtin_amdgcn_s_waitcnt(wait_vm(0));  // no load may still be writing LDS
     asm volatile("" ::: "memory");
 
-    // The four waves' results, unnormalised, row by row through LDS: float4 c of row
-    // r at slot c ^ (r % 16) of its row.
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int r = 16 * b + i16;
-      const float sum = quad_sum(l[b]);
-      if (g == 0) {
-        stat[0][wave][r] = m[b];
-        stat[1][wave][r] = sum;
-      }
-#pragma unroll
-      for (int db = 0; db < 8; ++db)
-        *reinterpret_cast<f32x4*>(mine + r * (kHeadDim * 4) + (((4 * db + g) ^ i16) << 4)) = o[db][b];
-    }
-    __syncthreads();
-    const bool part = step > 0 || stop < n_steps;
-    float* slot = p.slots + (2 * (size_t)blockIdx.x + (step > 0 ? 0 : 1)) * slot_floats(16 * NB);
-    for (int y = tid; y < 16 * NB * 16; y += kRowsThreads) {  // 8 values of a row each
-      const int r = y >> 4, c = (y & 15) * 2;
-      float top = kNoMax;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
-      float sum = 0.f;
-      f32x4 a0 = {}, a1 = {};
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float wk = __builtin_amdgcn_exp2f(stat[0][k][r] - top);
-        sum += wk * stat[1][k][r];
-        const unsigned char* row = smem + k * kWaveBytes + r * (kHeadDim * 4);
-        a0 += wk * *reinterpret_cast<const f32x4*>(row + ((c ^ (r & 15)) << 4));
-        a1 += wk * *reinterpret_cast<const f32x4*>(row + (((c + 1) ^ (r & 15)) << 4));
-      }
-      const bool live = top > 0.5f * kNoMax && sum > 0.f;  // false for a NaN too
-      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
-      const float lse = live ? top * kLn2 + logf(sum) : -INFINITY;
-      a0 *= inv;
-      a1 *= inv;
-      if (part) {
-        // A NaN among the scores is an LSE of NaN here: the merge tells it from a part without keys.
-        *reinterpret_cast<f32x4*>(slot + r * kHeadDim + 4 * c) = a0;
-        *reinterpret_cast<f32x4*>(slot + r * kHeadDim + 4 * c + 4) = a1;
-        if (c == 0) slot[16 * NB * kHeadDim + r] = sum != sum ? sum : lse;
-      } else if (r0 + r < rows) {
-        const int at = (int)((unsigned)(r0 + r) / (unsigned)p.G);
-        const int64_t out = (s.o_row + at) * p.Hq + kvh * p.G + (r0 + r - at * p.G);
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = (__bf16)a0[e];
-          v[4 + e] = (__bf16)a1[e];
-        }
-        *reinterpret_cast<bf16x8*>(p.o + out * kHeadDim + 4 * c) = v;
-        if (c == 0 && p.lse) p.lse[out] = lse;
-      }
-    }
-    if (last) return;
+    const bool last = same_walk(end, ShareStart{place, kvh, 0, 0});
+    more = !last && next_walk<false>(p, &x, &place, &kvh) && !same(end, ShareStart{place, kvh, 0, 0});
     step = 0;
-    if (!next_walk<false>(p, &x, &place, &kvh) || same(end, ShareStart{place, kvh, 0, 0})) return;
-    __syncthreads();  // the LDS is free for the next walk's tiles
   }
 }
 

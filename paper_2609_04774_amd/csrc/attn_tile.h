@@ -261,7 +261,7 @@ __device__ Share find_share(const PagedParams& p, int share) {
     u -= head * per_head + before * heads;
     if (u < 0 || u >= mine * heads) continue;
     for (int i = i0; i < i1; ++i) {
-      const int cost = cost_of(i);
+      const int cost = per == 1 ? (int)mine : cost_of(i);
       if (u >= (int64_t)cost * heads) {
         u -= (int64_t)cost * heads;
         continue;
