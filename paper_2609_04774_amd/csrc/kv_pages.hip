@@ -142,11 +142,16 @@ struct Want {
   int64_t first;
 };
 
-// Entries of a list that name sequence x before entry i, or (in a second list) at all.
+// Whether one of the first n entries of a list in LDS (16-byte aligned, readable up to
+// the next multiple of 8) is x.
 __device__ __forceinline__ bool named(const int32_t* list, int n, int x) {
-  for (int i = 0; i < n; ++i)
-    if (list[i] == x) return true;
-  return false;
+  bool hit = false;
+  for (int i = 0; i < n; i += 8) {
+    const i32x4 a = *reinterpret_cast<const i32x4*>(list + i), b = *reinterpret_cast<const i32x4*>(list + i + 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) hit |= ((a[k] == x) & (i + k < n)) | ((b[k] == x) & (i + 4 + k < n));
+  }
+  return hit;
 }
 
 struct ReserveList {
@@ -186,7 +191,7 @@ struct ForkList {
 // would depend on timing).
 template <class List, bool kFork>
 __global__ __launch_bounds__(kScanThreads) void take_pages_kernel(cp_kv_pool p, List list, int n, int32_t* missing) {
-  __shared__ int32_t seqs[CP_KV_MAX_LIST], second[kFork ? CP_KV_MAX_LIST : 1];
+  __shared__ __attribute__((aligned(16))) int32_t seqs[CP_KV_MAX_LIST], second[kFork ? CP_KV_MAX_LIST : 4];
   __shared__ int64_t need_end[CP_KV_MAX_LIST];  // pages that the entries up to this one want
   __shared__ int64_t wave_sum[kScanWaves];
   __shared__ int32_t n_missing;
