@@ -428,9 +428,9 @@ int cp_kv_gather(const void* k_cache, const void* v_cache, int64_t n_blocks, con
  * captured launch follows lengths and tables that change between replays.
  *   k_cache, v_cache  bf16 [n_blocks][16][n_heads_kv][128], 16-byte aligned.
  *   tables      int32 [n_seqs][table_stride]: the page of each 16 positions of
- *               a sequence.  An entry outside [0, n_blocks), and any position
- *               beyond 16 * table_stride, names no page: its keys and values
- *               read as zeros, and nothing is written through it.
+ *               a sequence.  An entry outside [0, n_blocks) names no page: its
+ *               keys and values read as zeros, and nothing is written through
+ *               it.  Positions from 16 * table_stride on have no keys.
  *   kv_len      int32 [n_seqs]: the positions of a sequence, its new tokens
  *               included (below 0 acts as 0, above 2^30 as 2^30).
  * New tokens come as rows: with q_start (device int32 [n_seqs + 1], ascending),

@@ -62,6 +62,8 @@ class Pool:
                 continue
             length = before[1][a]
             whole, part = divmod(length, B)
+            if part and whole < self.width and not 0 <= before[0][a][whole] < len(self.refs):
+                part = 0  # the parent's last page is not there: nothing to copy
             pages = None if out and part else self._take(1 if part else 0, None)
             if -(-length // B) > self.width:
                 pages, bad = None, True
@@ -78,10 +80,8 @@ class Pool:
             shared += [p for p in before[0][a][:whole] if 0 <= p < len(self.refs)]
             if part:
                 self.tables[c][whole], self.refs[pages[0]] = pages[0], 1
-                src = before[0][a][whole]
-                if 0 <= src < len(self.refs):
-                    for x in self.caches:
-                        x[pages[0]] = x[src]
+                for x in self.caches:
+                    x[pages[0]] = x[before[0][a][whole]]
         for p in shared:
             self.refs[p] += 1
         return missing

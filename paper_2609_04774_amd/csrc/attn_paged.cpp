@@ -1,6 +1,7 @@
 // Host side of attention over a paged cache: argument checks and kernel
 // parameters for cp_attn_paged and cp_attn_window (include/cp_attn.h).  Nothing is
 // planned here: the kernels cut the work by the lengths that they read.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <string>
@@ -61,15 +62,19 @@ int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspac
   if (!aligned(workspace, 256)) return fail(CP_ERR_INVALID, who + "workspace must be 256-byte aligned");
   if (workspace_bytes < need)
     return fail(CP_ERR_CAPACITY, who + "workspace needs " + std::to_string(need) + " bytes");
+  p->max_q = (int32_t)max_q;
   p->block_rows = block_rows(max_q, p->G);
   p->n_shares = shares_of(p->block_rows);
   p->blocks = (int32_t)((max_q * p->G + p->block_rows - 1) / p->block_rows);
   const int64_t places = (int64_t)p->n_segments * p->blocks;
   if (places > INT32_MAX / 2) return fail(CP_ERR_UNSUPPORTED, who + "too many sequences of so many rows");
-  // Blocks of a share, where each has several (of those that may have rows).
-  const int64_t full = p->n_rows * p->G / p->block_rows + p->n_segments;
-  const int64_t run = (full < places ? full : places) * p->Hkv / p->n_shares;
-  p->run = p->block_rows == kChunkRows && run > 1 ? (int32_t)run : 1;
+  // Blocks of a share, where each has several; not where most places have no rows
+  // (few long chunks among many sequences: those places are passed over in order).
+  // Against the order of the blocks themselves: rank 0 of a 32K prompt at degree 4
+  // 1977 us, 2132; through a window of 4096 433, 459.
+  const int64_t full = p->n_rows * p->G / p->block_rows;
+  const int64_t run = places * p->Hkv / p->n_shares;
+  p->run = p->block_rows == kChunkRows && run > 1 && 2 * full >= places ? (int32_t)run : 1;
   p->stride = (int32_t)((places + p->run - 1) / p->run);
   p->starts = static_cast<ShareStart*>(workspace);
   p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares));
@@ -143,16 +148,16 @@ extern "C" int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_str
     p.n_rows = n_rows;
     p.k_cache = static_cast<const unsigned char*>(kv->k_cache);
     p.v_cache = static_cast<const unsigned char*>(kv->v_cache);
-    p.n_blocks = (int32_t)(kv->n_blocks < INT32_MAX ? kv->n_blocks : INT32_MAX);
+    p.n_blocks = (int32_t)std::min<int64_t>(INT32_MAX, kv->n_blocks);
     p.tables = kv->tables;
     p.table_stride = kv->table_stride;
-    p.table_len = (int32_t)(kv->table_stride < INT32_MAX ? kv->table_stride : INT32_MAX);
+    p.table_len = (int32_t)std::min<int64_t>(INT32_MAX, kv->table_stride);
     p.paged_end = INT32_MAX;
+    p.key_end = (int32_t)std::min<int64_t>(kMaxTokens, kv->table_stride * kBlockTokens);
     p.n_segments = kv->n_seqs;
     p.q_start = q_start;
     p.kv_len = kv->kv_len;
     p.uniform_q = q_start ? 0 : (int32_t)max_q;
-    p.max_q = (int32_t)max_q;
     st = launch(&p, who, max_q, workspace, workspace_bytes, stream);
     if (st == CP_OK) clear_error();
     return st;
@@ -217,10 +222,11 @@ extern "C" int cp_attn_window(const cp_rank_plan* plan, const void* q, const voi
     p.n_rows = plan->n_rows;
     p.k_cache = static_cast<const unsigned char*>(k_cache);
     p.v_cache = static_cast<const unsigned char*>(v_cache);
-    p.n_blocks = (int32_t)(n_blocks < INT32_MAX ? n_blocks : INT32_MAX);
+    p.n_blocks = (int32_t)std::min<int64_t>(INT32_MAX, n_blocks);
     p.tables = block_table;
     p.table_len = (int32_t)(P / CP_KV_BLOCK_TOKENS);
     p.paged_end = (int32_t)P;
+    p.key_end = kMaxTokens;
     p.k_new = static_cast<const unsigned char*>(k_new);
     p.v_new = static_cast<const unsigned char*>(v_new);
     p.n_chunks = p.n_segments = 2;
@@ -231,7 +237,6 @@ extern "C" int cp_attn_window(const cp_rank_plan* plan, const void* q, const voi
       p.chunk_row[c] = x.local_offset;
       p.chunk_out[c] = out_order == CP_OUT_SEQUENCE ? x.q_begin - P : x.local_offset;
     }
-    p.max_q = (int32_t)plan->chunk_len;
     st = launch(&p, who, plan->chunk_len, workspace, workspace_bytes, stream);
     if (st == CP_OK) clear_error();
     return st;

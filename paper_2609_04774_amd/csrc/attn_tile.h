@@ -88,6 +88,7 @@ __device__ __forceinline__ Walk walk_of(const PagedParams& p, const Segment& s, 
   w.p_lo = s.pos0 + (int)((unsigned)r0 / (unsigned)p.G);
   w.p_hi = s.pos0 + (int)((unsigned)(r1 - 1) / (unsigned)p.G);
   w.end = w.p_hi + 1 > 0 ? w.p_hi + 1 : 0;
+  w.end = w.end < p.key_end ? w.end : p.key_end;
   w.lo = 0;
   w.sink = 0;
   w.n_sink_tiles = 0;
@@ -99,7 +100,7 @@ __device__ __forceinline__ Walk walk_of(const PagedParams& p, const Segment& s, 
     w.base = w.lo & ~(kBlockTokens - 1);
     if (w.n_sink_tiles && w.base <= w.n_sink_tiles * kTileKeys) w.n_sink_tiles = w.base = 0;
   }
-  w.n = w.n_sink_tiles + (w.end - w.base + kTileKeys - 1) / kTileKeys;
+  w.n = w.n_sink_tiles + (w.end > w.base ? (w.end - w.base + kTileKeys - 1) / kTileKeys : 0);
   return w;
 }
 
@@ -116,7 +117,7 @@ __device__ __forceinline__ bool whole_tile(const Walk& w, int t0) {
   return t0 + kTileKeys <= w.end && (t0 >= w.lo || t0 + kTileKeys <= w.sink);
 }
 __device__ __forceinline__ bool open_tile(const PagedParams& p, const Walk& w, int t0) {
-  return t0 + kTileKeys <= w.p_lo + 1 &&
+  return t0 + kTileKeys <= w.p_lo + 1 && t0 + kTileKeys <= w.end &&
          (!p.window || t0 > w.p_hi - p.window || t0 + kTileKeys <= p.n_sink);
 }
 
@@ -124,7 +125,7 @@ __device__ __forceinline__ bool open_tile(const PagedParams& p, const Walk& w, i
 __device__ __forceinline__ void open_tiles(const PagedParams& p, const Walk& w, int* first, int* end) {
   const int below = p.window ? w.p_hi - p.window + 1 - w.base : 0;  // keys from base on that some row does not see
   const int a = w.n_sink_tiles + (below > 0 ? (below + kTileKeys - 1) / kTileKeys : 0);
-  const int keys = w.p_lo + 1 - w.base;
+  const int keys = (w.p_lo + 1 < w.end ? w.p_lo + 1 : w.end) - w.base;
   const int b = w.n_sink_tiles + (keys > 0 ? keys / kTileKeys : 0);
   *first = a < w.n ? a : w.n;
   *end = b > *first ? b : *first;
@@ -170,6 +171,7 @@ struct Block {
   Segment s;
   int block;
   bool rows;  // it has any
+  int next;   // the first place after this one whose block may have rows
 };
 
 __device__ __forceinline__ Block block_at(const PagedParams& p, int place) {
@@ -178,9 +180,12 @@ __device__ __forceinline__ Block block_at(const PagedParams& p, int place) {
   const int seg = p.blocks == 1 ? i : (int)((unsigned)i / (unsigned)p.blocks);
   x.block = i - seg * p.blocks;
   x.rows = false;
+  x.next = place + 1;
   if (seg < p.n_segments) {
     x.s = segment_at(p, seg);
-    x.rows = (int64_t)x.block * p.block_rows < (int64_t)x.s.n * p.G;
+    const int64_t left = (int64_t)x.s.n * p.G - (int64_t)x.block * p.block_rows;
+    x.rows = left > 0;
+    if (p.run == 1 && left <= p.block_rows) x.next = (seg + 1) * p.blocks;  // the segment's last one
   }
   return x;
 }
@@ -193,7 +198,8 @@ __device__ __forceinline__ bool next_walk(const PagedParams& p, Block* x, int* p
     *kvh = 0;
   }
   do {
-    if (++*place >= places(p)) {
+    *place = x->next;
+    if (*place >= places(p)) {
       if (!kHeadsOuter || ++*kvh >= p.Hkv) return false;
       *place = 0;
     }
@@ -227,12 +233,13 @@ __device__ Share find_share(const PagedParams& p, int share) {
   const int per = (n_places + kThreads - 1) / kThreads;
   const int i0 = tid * per < n_places ? tid * per : n_places;
   const int i1 = i0 + per < n_places ? i0 + per : n_places;
-  auto cost_of = [&](int place) {
-    const Block x = block_at(p, place);
-    return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, x.s, x.block)) : 0;
-  };
+  auto cost_of = [&](const Block& x) { return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, x.s, x.block)) : 0; };
   int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += cost_of(i);
+  for (int i = i0; i < i1;) {
+    const Block x = block_at(p, i);
+    mine += cost_of(x);
+    i = x.next;
+  }
   int64_t before = mine;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) {
@@ -260,8 +267,14 @@ __device__ Share find_share(const PagedParams& p, int share) {
     const int head = kHeadsOuter ? (int)quotient(u, per_head) : 0;
     u -= head * per_head + before * heads;
     if (u < 0 || u >= mine * heads) continue;
-    for (int i = i0; i < i1; ++i) {
-      const int cost = per == 1 ? (int)mine : cost_of(i);
+    for (int i = i0, next; i < i1; i = next) {
+      int cost = (int)mine;
+      next = i + 1;
+      if (per > 1) {
+        const Block x = block_at(p, i);
+        cost = cost_of(x);
+        next = x.next;
+      }
       if (u >= (int64_t)cost * heads) {
         u -= (int64_t)cost * heads;
         continue;
@@ -270,9 +283,9 @@ __device__ Share find_share(const PagedParams& p, int share) {
       int place = i, kvh = head + k, step = (int)(u - (int64_t)k * cost) - kSetup;
       if (step < kSnap) step = 0;
       if (step && cost - kSetup - step < kSnap) {
-        Block next;
+        Block x = block_at(p, i);
         step = 0;
-        if (!next_walk<kHeadsOuter>(p, &next, &place, &kvh)) place = n_places, kvh = 0;
+        if (!next_walk<kHeadsOuter>(p, &x, &place, &kvh)) place = n_places, kvh = 0;
       }
       found[e] = ShareStart{place, kvh, step, 0};
       break;
@@ -294,7 +307,7 @@ __device__ __forceinline__ uint32_t lds_addr(const unsigned char* p) {
 }
 
 // 256 zero bytes: what a key without a page, or that no row sees, reads.
-__device__ __attribute__((aligned(256))) unsigned char g_zeros[kRowBytes];
+static __device__ __attribute__((aligned(256))) unsigned char g_zeros[kRowBytes];
 
 // One direct-to-LDS load: lane l's 16 bytes at its address land at LDS byte lds_base
 // + 16 l.  Inline assembly, so that the compiler does not make every later LDS
@@ -378,6 +391,11 @@ __device__ __forceinline__ float quad_sum(float x) {
 __device__ __forceinline__ void mask_scores(const PagedParams& p, f32x4 (&s)[2], int t0, int g, int pos) {
   const unsigned window = p.window ? (unsigned)p.window : 1u << 31;
   const int away = pos - (t0 + 4 * g);
+  if (__builtin_expect(t0 + kTileKeys > p.key_end, 0)) {  // no keys from there on
+    const int end = p.key_end - (t0 + 4 * g);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s[c >> 2][c & 3] = 16 * (c >> 2) + (c & 3) < end ? s[c >> 2][c & 3] : -INFINITY;
+  }
   if (__builtin_expect(p.window && t0 < p.n_sink, 0)) {
     const int sinks = p.n_sink - (t0 + 4 * g);
 #pragma unroll

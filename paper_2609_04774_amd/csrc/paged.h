@@ -27,7 +27,8 @@ struct PagedParams {
   int32_t table_len;       // entries of a table
   const int32_t* tables;
   int64_t table_stride;
-  int32_t paged_end;       // positions below it are read through the table,
+  int32_t paged_end;       // positions below it are read through the table
+  int32_t key_end;         // and from this one on there are no keys
 
   // A batch: sequence s has rows q_start[s] .. q_start[s + 1] (or uniform_q each),
   // the last of its kv_len[s] positions.

@@ -124,13 +124,33 @@ def test_pages_that_name_nothing_read_as_zeros():
     b.check(*b.run())
 
 
-def test_positions_beyond_the_table_read_as_zeros():
-    b = Batch([64], [1], 8, 2, seed=76, uniform=True, table_extra=0)
-    b.dev_len.fill_(100)
-    b.k[0] = torch.cat([b.k[0], torch.zeros(36, 2, D, dtype=torch.bfloat16)])
-    b.v[0] = torch.cat([b.v[0], torch.zeros(36, 2, D, dtype=torch.bfloat16)])
-    b.kv_len = [100]
-    b.check(*b.run())
+@pytest.mark.parametrize("new", [1, 4, 60])
+def test_positions_beyond_the_table_have_no_keys(new):
+    """A length that its table does not cover: the rows at its end see what the
+    table holds (an odd number of pages: half a tile)."""
+    b = Batch([80, 40], [new, new], 8, 2, seed=76, uniform=True, table_extra=0)
+    o, lse = torch.empty(2 * new, 8, D, dtype=torch.bfloat16, device=DEV), torch.empty(2 * new, 8, device=DEV)
+    ws = torch.empty(cp.attn_paged_workspace_size(b.kv, 2 * new, new, 8), dtype=torch.uint8, device=DEV)
+    for length in (100, 2**31 - 1):
+        for window, n_sink in ((0, 0), (120, 3), (33, 20)):
+            b.dev_len[0] = length
+            cp.attn_paged(b.kv, b.q.to(DEV), o, ws, lse=lse, window=window, n_sink=n_sink)
+            pos = min(length, 2**30) - new + np.arange(new)
+            want = owin.attend(f64(b.q)[:new], pos, f64(b.k[0]), f64(b.v[0]), np.arange(80), window, n_sink)
+            compare(f64(o)[:new], f64(lse)[:new], want, 80, f"length {length}, window {window}")
+            want = owin.attend(f64(b.q)[new:], b.positions(1), f64(b.k[1]), f64(b.v[1]), np.arange(40), window, n_sink)
+            compare(f64(o)[new:], f64(lse)[new:], want, 40, "the other sequence")
+
+
+def test_a_long_chunk_among_many_sequences():
+    """Most sequences have one row, one has many, some none, in any order."""
+    rng = np.random.RandomState(6)
+    new = [1] * 300
+    new[7], new[150], new[299] = 700, 0, 40
+    lens = [n + int(x) for n, x in zip(new, rng.randint(0, 90, 300))]
+    b = Batch(lens, new, 8, 1, seed=82)
+    b.check(*b.run(), rows=np.array([0, 1, 31, 32, 300, 699]))
+    b.check(*b.run(50, 4), 50, 4, rows=np.array([0, 1, 31, 32, 300, 699]))
 
 
 def test_scale_and_strided_queries():

@@ -89,6 +89,13 @@ def test_fork_and_free():
     b.free([6], [0], [2**31 - 1])
 
 
+def test_fork_of_a_parent_whose_pages_are_partly_gone():
+    b = Both(6, 8, 40, seed=9)
+    b.reserve([0, 1], [70, 45])
+    b.free([0, 1], [16, 32], [64, 45])                # pages in the middle; the last one, filled in part
+    b.fork([0, 1], [2, 3])
+
+
 def test_fork_without_pages_left():
     b = Both(6, 4, 5, seed=2)
     b.reserve([0, 1], [20, 32])                       # 4 of 5 pages
