@@ -219,13 +219,19 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   Walk w;
   int step = 0, n = 0;  // the part's first tile, and its tiles
   int open0 = 0, open1 = 0;  // tiles of the walk that every row of the block sees whole
-  int ids = -1, ids_of = -64;  // pages of this wave's half of 64 tiles, one per lane
+  int ids = -1, ids_of = 0;  // pages of this wave's half of 64 tiles, one per lane
   int pos[NB];
   bf16x8 qf[NB][4];
   f32x4 o[8][NB];
   float m[NB], l[NB];
   bf16x8 pf[NB];
 
+  auto fetch_ids = [&](int j) {
+    ids_of = j;
+    ids = -1;
+    if (j + lane < n) ids = page_of(p, s, tile_begin(w, step + j + lane) + load_half * kBlockTokens);
+    landed(ids);
+  };
   // Tile j of the part into buffer j % kBufs; past the last it is loaded again, into
   // a buffer nobody reads, so that the waits can count.
   auto load = [&](int j) {
@@ -233,11 +239,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
     const int jj = j < n ? j : n - 1;
     const int t0 = tile_begin(w, step + jj);
     const int hp = t0 + load_half * kBlockTokens;
-    if (__builtin_expect((jj & ~63) != ids_of, 0)) {
-      ids_of = jj & ~63;
-      ids = -1;
-      if (ids_of + lane < n) ids = page_of(p, s, tile_begin(w, step + ids_of + lane) + load_half * kBlockTokens);
-    }
+    if (__builtin_expect((jj & ~63) != ids_of, 0)) fetch_ids(jj & ~63);
     const HalfSource h = half_source(p, __builtin_amdgcn_readlane(ids, jj & 63), hp, kvh);
     const unsigned char* kb = (h.paged ? p.k_cache : p.k_new) + h.offset;
     const unsigned char* vb = (h.paged ? p.v_cache : p.v_new) + h.offset;
@@ -325,7 +327,11 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         for (int d = 0; d < 4; ++d) qf[b][d] = *reinterpret_cast<const bf16x8*>(from + 32 * d);
       }
       open_tiles(p, w, &open0, &open1);
-      ids_of = -64;
+      fetch_ids(0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) landed(qf[b][d]);
       if (n > 0)
         for (int j = 0; j < kAhead; ++j) load(j);
     }

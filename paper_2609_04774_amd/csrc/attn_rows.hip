@@ -194,6 +194,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     if (!first) store();
     if (!more) return;
     out = now;
+    landed(ids);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) landed(qf[b][d]);
     int ids_of = 0;
     if (n_mine > 0) {
       load(0, 0);
@@ -215,6 +220,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       if ((jn & ~31) != ids_of) {
         ids_of = jn & ~31;
         fetch_ids(ids_of);
+        landed(ids);
       }
       __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // K of tile j is in LDS
       asm volatile("" ::: "memory");

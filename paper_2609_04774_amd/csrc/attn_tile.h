@@ -321,6 +321,14 @@ __device__ __forceinline__ void load_lds_from(const void* addr, uint32_t lds_bas
       : "memory");
 }
 
+// A loaded value is waited for here, and not where it is used: in a loop that would
+// be a wait for every load in flight, the direct ones among them, each time around
+// (the compiler cannot tell whether the value was loaded in this iteration).
+template <class T>
+__device__ __forceinline__ void landed(T& x) {
+  asm volatile("" : "+v"(x));
+}
+
 // s_waitcnt immediate: at most n of this wave's vector-memory operations
 // outstanding (vmcnt[3:0] at [3:0], vmcnt[5:4] at [15:14]).
 constexpr int wait_vm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
