@@ -23,12 +23,14 @@ namespace {
 using namespace tile;
 
 constexpr int kWaves = kChunkThreads / 64;
-constexpr int NB = 2;      // blocks of 16 rows per wave
-static_assert(16 * NB * kWaves == kChunkRows, "the rows of a workgroup");
 constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % kBufs
 constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
 constexpr int kSetup = 10;  // of a walk, in tiles
 constexpr int kSnap = 4;   // tiles: a part costs its set-up, and its rows a merge
+// A wide block's tile takes 11/8 of a narrow one's (0.93 us).  A share of wide blocks
+// costs more besides, in tiles: its set-ups and its parts' merge are larger, and so
+// are, at both edges of a window, the tiles that some row sees in part.
+constexpr int kWideSteps = 40, kWideWindowSteps = 80;
 
 // LDS tiles by 16-byte columns: column c of a half holds chunk c of its 16 keys, key
 // k at slot k ^ 8 (c % 2).  The K reads (16 keys of a column) and the transposed V
@@ -69,8 +71,10 @@ __device__ __forceinline__ void pin(const T& x) {  // computed before this point
   asm volatile("" ::"v"(x));
 }
 
+template <int NB>
 using Scores = f32x4[NB][2];  // [block][half]
 
+template <int NB>
 struct Weights {
   float sum[NB];     // fp32 sums of this lane's weights
   bf16x2 pair[NB][4];
@@ -80,10 +84,9 @@ constexpr float kMaxSum = 65536.f;  // of a lane's 8 weights of a tile; beyond i
 
 // One unit of a tile's softmax (of 12 NB, about equal): two exponentials of a pair
 // of scores, or the pair's rounding and sum.
-__device__ __forceinline__ void softmax_unit(int u, Scores& s, Weights& w, const float (&m)[NB], float sl2) {
+template <int NB>
+__device__ __forceinline__ void softmax_unit(int u, Scores<NB>& s, Weights<NB>& w, const float (&m)[NB], float sl2) {
   const int b = u / 12, t = u % 12 / 3, kind = u % 3;  // block, pair
-
-
   const int half = t >> 1, r = 2 * (t & 1);
   if (kind < 2) {
     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][half][r + kind], sl2, -m[b]));
@@ -97,21 +100,24 @@ __device__ __forceinline__ void softmax_unit(int u, Scores& s, Weights& w, const
   }
 }
 
-__device__ __forceinline__ void qk_step(Scores& s, const bf16x8& k, const bf16x8 (&qf)[NB][4], int q) {
+template <int NB>
+__device__ __forceinline__ void qk_step(Scores<NB>& s, const bf16x8& k, const bf16x8 (&qf)[NB][4], int q) {
 #pragma unroll
   for (int b = 0; b < NB; ++b)
     s[b][q & 1] = mfma16(k, qf[b][q >> 1], (q >> 1) == 0 ? f32x4{} : s[b][q & 1]);
 }
 
+template <int NB>
 __device__ __forceinline__ void qk_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&qf)[NB][4],
-                                        Scores& s) {
+                                        Scores<NB>& s) {
 #pragma unroll
   for (int q = 0; q < 8; ++q) qk_step(s, load_k(buf, f, q), qf, q);
 }
 
 // Raises the running maxima to a tile's own where that is higher; O and the sums
 // follow.
-__device__ __forceinline__ void raise_max(const Scores& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
+template <int NB>
+__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     float top = s[b][0][0];
@@ -127,7 +133,8 @@ __device__ __forceinline__ void raise_max(const Scores& s, float (&m)[NB], float
 }
 
 // The weights become the operand of the second product.
-__device__ __forceinline__ void finish(const Weights& w, float (&l)[NB], bf16x8 (&pf)[NB]) {
+template <int NB>
+__device__ __forceinline__ void finish(const Weights<NB>& w, float (&l)[NB], bf16x8 (&pf)[NB]) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     l[b] += w.sum[b];
@@ -137,6 +144,7 @@ __device__ __forceinline__ void finish(const Weights& w, float (&l)[NB], bf16x8 
   }
 }
 
+template <int NB>
 __device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&pf)[NB],
                                         f32x4 (&o)[8][NB]) {
 #pragma unroll
@@ -150,6 +158,7 @@ __device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragment
 // The order of the units over an iteration: the exponentials of all blocks but the
 // last first, and the roundings from slot 8 on, when the products with the tile
 // before have freed their operand's registers.
+template <int NB>
 struct Order {
   int unit[12 * NB];
   constexpr Order() : unit{} {
@@ -167,20 +176,42 @@ struct Order {
       for (int k = t < te ? 2 : 0; k < 3; ++k) unit[n++] = last + 3 * t + k;
   }
 };
-constexpr Order kOrder{};
+template <int NB>
+constexpr Order<NB> kOrder{};
 
-constexpr int kLookahead = 3;  // slots a fragment is read ahead of its products
 
+__device__ __forceinline__ Walk uniform_walk(const Walk& w) {
+  auto u = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  return Walk{u(w.end), u(w.lo), u(w.sink), u(w.p_lo), u(w.p_hi), u(w.n_sink_tiles), u(w.base), u(w.n)};
+}
+
+// Of a launch that may have wide blocks (p.wide) the kernel of narrow ones comes first,
+// and the lengths say which of the two does the work.
+template <int NB>
 __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParams p) {
+  constexpr int kRows = 16 * NB * kWaves;
+  constexpr int kLookahead = NB == 2 ? 3 : 2;  // slots a fragment is read ahead of its products
+  constexpr bool kWide = kRows == kWideRows;
+  static_assert(kWide || kRows == kChunkRows, "the rows of a workgroup");
   // The buffers of K, of V, and a V tile of zeros.
   __shared__ __attribute__((aligned(1024))) unsigned char smem[(2 * kBufs + 1) * kTileBytes];
+  __shared__ int64_t wave_sum[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
+  const Blocks blocks = kWide ? p.wide : p.narrow;
+  if (kWide && *p.choice == 0) return;
   // Shares are numbered so that an XCD's workgroups (every eighth) have neighbouring
   // ones, whose walks meet in its L2.
   const int number = p.n_shares % 8 == 0 ? (int)(blockIdx.x % 8) * (p.n_shares / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
-  const Share share = find_share<kChunkThreads, 1, kSetup, kSnap, true>(p, number);
+  const Counted counted = count_steps<kChunkThreads, 1, kSetup>(p, blocks, wave_sum[0]);
+  if (!kWide && p.choice) {
+    const Counted other = count_steps<kChunkThreads, 1, kSetup>(p, p.wide, wave_sum[1]);
+    const bool wide = other.total * 11 / 8 * p.Hkv + (p.window ? kWideWindowSteps : kWideSteps) * p.n_shares < counted.total * p.Hkv;
+    if (blockIdx.x == 0 && tid == 0) *p.choice = wide;
+    if (wide) return;
+  }
+  const Share share = find_share<1, kSetup, kSnap, true>(p, blocks, counted, number);
   if (tid == 0) p.starts[number] = share.at;
   if (same(share.at, share.end)) return;
 
@@ -205,7 +236,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   const ShareStart at = uniform(share.at), end = uniform(share.end);
   bool ahead = end.step > 0 && !same_walk(at, end);
   int place = ahead ? end.place : at.place, kvh = ahead ? end.kvh : at.kvh;
-  Block x = block_at(p, place);
+  Block x = block_at(p, blocks, place);
   const Segment& s = x.s;
 
   // One part of a walk after another.  While the rows of one are stored, the queries
@@ -254,7 +285,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
     }
   };
   auto closed = [&](int j) { return (step + j < open0) | (step + j >= open1); };
-  auto mask = [&](int j, Scores& sc) {
+  auto mask = [&](int j, Scores<NB>& sc) {
     if (__builtin_expect(!closed(j), 1)) return;
     const int t0 = tile_begin(w, step + j);
 #pragma unroll
@@ -283,7 +314,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         for (int db = 0; db < 8; ++db)
           *reinterpret_cast<f32x4*>(out.slot + rb * kHeadDim + 16 * db + 4 * g) = o[db][b] * inv;
         // A NaN among the scores is an LSE of NaN here: the merge tells it from a part without keys.
-        if (g == 0) out.slot[p.block_rows * kHeadDim + rb] = sum != sum ? sum : lse;
+        if (g == 0) out.slot[kRows * kHeadDim + rb] = sum != sum ? sum : lse;
       } else if (r < out.rows) {
         const int q = (int)((unsigned)r / (unsigned)p.G);
         const int64_t row = (out.o_row + q) * p.Hq + out.kvh * p.G + (r - q * p.G);
@@ -304,17 +335,17 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
     const ShareStart here = {place, kvh, 0, 0};
     Rows now = out;
     if (more) {
-      w = block_walk(p, s, x.block);
+      w = uniform_walk(block_walk(p, blocks, s, x.block));
       const int n_steps = steps_of<1>(w);
       step = same_walk(here, at) ? at.step : 0;
       const int stop = same_walk(here, end) ? end.step : n_steps;
       n = w.n ? stop - step : 0;
       now.o_row = s.o_row;
       now.rows = s.n * p.G;
-      now.r0 = x.block * p.block_rows + 16 * NB * wave;
+      now.r0 = x.block * kRows + 16 * NB * wave;
       now.kvh = kvh;
       now.slot = step > 0 || stop < n_steps
-                     ? p.slots + (2 * (size_t)number + (step > 0 ? 0 : 1)) * slot_floats(p.block_rows)
+                     ? p.slots + (2 * (size_t)number + (step > 0 ? 0 : 1)) * slot_floats(kRows)
                      : nullptr;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -357,8 +388,8 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         __syncthreads();
         const unsigned char* k_now = kbuf + (j & (kBufs - 1)) * kTileBytes;
         const unsigned char* v_now = vbuf + (j & (kBufs - 1)) * kTileBytes;
-        Scores sa, sb;
-        Weights wt;
+        Scores<NB> sa, sb;
+        Weights<NB> wt;
         if (active) {
           qk_tile(k_now, fr, qf, sa);
           mask(j, sa);
@@ -379,13 +410,10 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         // is zeros.
         bf16x8 pre[kLookahead];
         const unsigned char* v_before = vzero;
-        if (active) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b) pf[b] = bf16x8{};
-#pragma unroll
-          for (int x = 0; x < kLookahead; ++x) pre[x] = load_v(vzero, fr, x);
-        }
-        auto iteration = [&](int j, Scores& s_in, Scores& s_out) {
+        Fragments at_lane = fr;  // (spilled around the loop at most)
+        landed(at_lane.k);
+        landed(at_lane.v);
+        auto iteration = [&](int j, Scores<NB>& s_in, Scores<NB>& s_out) {
           const unsigned char* k_next = kbuf + ((j + 1) & (kBufs - 1)) * kTileBytes;
           const unsigned char* v_this = vbuf + (j & (kBufs - 1)) * kTileBytes;
           load(j + kAhead);
@@ -396,11 +424,11 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
           for (int slot = 0; slot < 16; ++slot) {
             const int x = slot + kLookahead;
             if (x < 8)
-              f[x] = load_v(v_before, fr, x);
+              f[x] = load_v(v_before, at_lane, x);
             else if (x < 16)
-              f[x] = load_k(k_next, fr, x - 8);
+              f[x] = load_k(k_next, at_lane, x - 8);
             else
-              pre[x - 16] = load_v(v_this, fr, x - 16);
+              pre[x - 16] = load_v(v_this, at_lane, x - 16);
             if (slot < 8) {
 #pragma unroll
               for (int b = 0; b < NB; ++b) o[slot][b] = mfma16(f[slot], pf[b], o[slot][b]);
@@ -409,7 +437,7 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
             }
 #pragma unroll
             for (int u = slot * 12 * NB / 16; u < (slot + 1) * 12 * NB / 16; ++u)
-              softmax_unit(kOrder.unit[u], s_in, wt, m, sl2);
+              softmax_unit(kOrder<NB>.unit[u], s_in, wt, m, sl2);
             __builtin_amdgcn_sched_barrier(0);
           }
           bool fine = true;
@@ -429,6 +457,10 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
         // every tile up to j + 2 has landed, and the buffers that its loads fill were
         // last read before it.
         if (active) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) pf[b] = bf16x8{};
+#pragma unroll
+          for (int x = 0; x < kLookahead; ++x) pre[x] = load_v(vzero, at_lane, x);
           for (;;) {
             __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));
             __syncthreads();
@@ -458,9 +490,9 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
       ahead = false;
       place = at.place;
       kvh = at.kvh;
-      x = block_at(p, place);
+      x = block_at(p, blocks, place);
     } else {
-      more = !same_walk(here, end) && next_walk<true>(p, &x, &place, &kvh) &&
+      more = !same_walk(here, end) && next_walk<true>(p, blocks, &x, &place, &kvh) &&
              !same_walk(end, ShareStart{place, kvh, 0, 0});
     }
     __syncthreads();  // every wave is done with the buffers
@@ -471,7 +503,9 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
 
 int launch_attn_chunk(const PagedParams& p, void* stream, const char* who) {
   const dim3 grid((unsigned)p.n_shares), block(kChunkThreads);
-  hipLaunchKernelGGL(attn_chunk_kernel, grid, block, 0, (hipStream_t)stream, p);
+  hipStream_t st = (hipStream_t)stream;
+  hipLaunchKernelGGL(attn_chunk_kernel<kChunkRows / (16 * kWaves)>, grid, block, 0, st, p);
+  if (p.choice) hipLaunchKernelGGL(attn_chunk_kernel<kWideRows / (16 * kWaves)>, grid, block, 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));
   return launch_attn_merge(p, stream, who);

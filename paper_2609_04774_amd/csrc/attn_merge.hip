@@ -28,11 +28,12 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
   const ShareStart at = p.starts[share];
   ShareStart next = share + 1 + lane < p.n_shares ? p.starts[share + 1 + lane] : none;
   if (at.step == 0 || (same_walk(before, at) && before.step > 0)) return;
-  const Block x = block_at(p, at.place);
+  const Blocks& b = p.choice && *p.choice ? p.wide : p.narrow;
+  const Block x = block_at(p, b, at.place);
   const Segment& s = x.s;
   const int r0 = kRows * (4 * blockIdx.y + (threadIdx.x >> 6));  // of the block
-  const int rows = s.n * p.G - x.block * p.block_rows;
-  if (r0 >= rows) return;
+  const int rows = s.n * p.G - x.block * b.rows;
+  if (r0 >= rows || r0 >= b.rows) return;
   int n = 2;  // parts
   for (;;) {
     const uint64_t in = __builtin_amdgcn_ballot_w64(same_walk(next, at) && next.step > 0);
@@ -43,9 +44,9 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
     n += 64;
     next = share + n - 1 + lane < p.n_shares ? p.starts[share + n - 1 + lane] : none;
   }
-  const size_t size = slot_floats(p.block_rows);
+  const size_t size = slot_floats(b.rows);
   auto slot_of = [&](int k) { return p.slots + (2 * (size_t)(share - 1 + k) + (k == 0 ? 1 : 0)) * size; };
-  auto lse_of = [&](int k, int r) { return slot_of(k)[(size_t)p.block_rows * kHeadDim + r]; };
+  auto lse_of = [&](int k, int r) { return slot_of(k)[(size_t)b.rows * kHeadDim + r]; };
   float top[kRows], sum[kRows];
   float2 acc[kRows];
 #pragma unroll
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
     for (int k = 1; k < 64; k *= 2) sum[i] += __shfl_xor(sum[i], k);
     if (r0 + i >= rows) continue;
     const float inv = top[i] == -INFINITY ? 0.f : 1.f / sum[i];
-    const int row = x.block * p.block_rows + r0 + i;
+    const int row = x.block * b.rows + r0 + i;
     const int q = (int)((unsigned)row / (unsigned)p.G);
     const int64_t out = (s.o_row + q) * p.Hq + at.kvh * p.G + (row - q * p.G);
     reinterpret_cast<bf16x2*>(p.o + out * kHeadDim)[lane] = bf16x2{(__bf16)(acc[i].x * inv), (__bf16)(acc[i].y * inv)};
@@ -109,11 +110,11 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
 int launch_attn_merge(const PagedParams& p, void* stream, const char* who) {
   if (p.n_shares == 1) return CP_OK;
   const unsigned shares = (unsigned)p.n_shares - 1;
-  if (p.block_rows > 32)  // few parts of many rows
-    hipLaunchKernelGGL(share_merge_kernel<4>, dim3(shares, (unsigned)(p.block_rows / 16)), dim3(256), 0,
+  if (p.narrow.rows > 32)  // few parts of many rows
+    hipLaunchKernelGGL(share_merge_kernel<4>, dim3(shares, (unsigned)((p.choice ? p.wide.rows : p.narrow.rows) / 16)), dim3(256), 0,
                        (hipStream_t)stream, p);
   else
-    hipLaunchKernelGGL(share_merge_kernel<1>, dim3(shares, (unsigned)(p.block_rows / 4)), dim3(256), 0,
+    hipLaunchKernelGGL(share_merge_kernel<1>, dim3(shares, (unsigned)(p.narrow.rows / 4)), dim3(256), 0,
                        (hipStream_t)stream, p);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CP_OK : fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));

@@ -32,8 +32,8 @@ int set_common(PagedParams* p, const std::string& who, int32_t Hq, int32_t Hkv, 
   p->Hq = Hq;
   p->Hkv = Hkv;
   p->G = Hq / Hkv;
-  p->scale = scale > 0.f ? scale : 1.f / std::sqrt((float)head_dim);
-  p->scale_log2 = p->scale * 1.4426950408889634f;
+  p->scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)head_dim)) * 1.4426950408889634f;
+  if (std::isinf(p->scale_log2)) return fail(CP_ERR_INVALID, who + "softmax_scale is too large");
   // No position is beyond 2^30: a longer window shows every key.
   p->window = window >= kMaxTokens ? 0 : (int32_t)window;
   p->n_sink = (int32_t)(n_sink < kMaxTokens ? n_sink : kMaxTokens);
@@ -49,37 +49,61 @@ int block_rows(int64_t max_q, int32_t G) {
 }
 int shares_of(int block_rows) { return block_rows == kChunkRows ? kChunkShares : kRowsShares; }
 
-size_t starts_bytes(int shares) { return ((size_t)shares * sizeof(ShareStart) + 255) / 256 * 256; }
-
-size_t workspace_bytes_of(int64_t max_q, int32_t G) {
-  const int rows = block_rows(max_q, G);
-  return starts_bytes(shares_of(rows)) + 2 * (size_t)shares_of(rows) * slot_floats(rows) * 4;
+// Whether wide blocks (the lengths decide on them) are worth a second kernel's launch, 4 us
+// where it has nothing to do.  One prompt's 4096 rows of 32 and 8 heads with and without
+// the choice: alone 176 and 173 us, after 8K tokens 608 and 642, after 32K 1875 and 2049;
+// 2048 rows alone 84 and 80, after 8K 315 and 316, after 32K 978 and 1016.
+bool may_be_wide(int block_rows, int64_t n_rows, int32_t Hq) {
+  return block_rows == kChunkRows && n_rows * Hq >= 131072;
 }
 
-int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspace, size_t workspace_bytes, void* stream) {
-  const size_t need = workspace_bytes_of(max_q, p->G);
-  if (!workspace) return fail(CP_ERR_INVALID, who + "workspace is NULL");
-  if (!aligned(workspace, 256)) return fail(CP_ERR_INVALID, who + "workspace must be 256-byte aligned");
-  if (workspace_bytes < need)
-    return fail(CP_ERR_CAPACITY, who + "workspace needs " + std::to_string(need) + " bytes");
-  p->max_q = (int32_t)max_q;
-  p->block_rows = block_rows(max_q, p->G);
-  p->n_shares = shares_of(p->block_rows);
-  p->blocks = (int32_t)((max_q * p->G + p->block_rows - 1) / p->block_rows);
-  const int64_t places = (int64_t)p->n_segments * p->blocks;
-  if (places > INT32_MAX / 2) return fail(CP_ERR_UNSUPPORTED, who + "too many sequences of so many rows");
+// The shares' starts and, behind them, the choice of blocks.
+size_t starts_bytes(int shares) { return ((size_t)shares * sizeof(ShareStart) + 255) / 256 * 256 + 256; }
+
+size_t workspace_bytes_of(int64_t n_rows, int64_t max_q, int32_t Hq, int32_t G) {
+  const int rows = block_rows(max_q, G);
+  return starts_bytes(shares_of(rows)) +
+         2 * (size_t)shares_of(rows) * slot_floats(may_be_wide(rows, n_rows, Hq) ? kWideRows : rows) * 4;
+}
+
+// How a launch is cut into blocks of so many rows.
+Blocks cut(const PagedParams& p, int rows) {
+  Blocks b;
+  b.rows = rows;
+  b.n = (int32_t)(((int64_t)p.max_q * p.G + rows - 1) / rows);
+  const int64_t places = (int64_t)p.n_segments * b.n;
   // Blocks of a share, where each has several; not where most places have no rows
   // (few long chunks among many sequences: those places are passed over in order).
   // Against the order of the blocks themselves: rank 0 of a 32K prompt at degree 4
   // 1977 us, 2132; through a window of 4096 433, 459.
-  const int64_t full = p->n_rows * p->G / p->block_rows;
-  const int64_t run = places * p->Hkv / p->n_shares;
-  p->run = p->block_rows == kChunkRows && run > 1 && 2 * full >= places ? (int32_t)run : 1;
-  p->stride = (int32_t)((places + p->run - 1) / p->run);
+  const int64_t full = p.n_rows * p.G / rows;
+  const int64_t run = places * p.Hkv / p.n_shares;
+  b.run = rows >= kChunkRows && run > 1 && 2 * full >= places ? (int32_t)run : 1;
+  b.stride = (int32_t)((places + b.run - 1) / b.run);
+  return b;
+}
+
+int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspace, size_t workspace_bytes, void* stream) {
+  const size_t need = workspace_bytes_of(p->n_rows, max_q, p->Hq, p->G);
+  if (!workspace) return fail(CP_ERR_INVALID, who + "workspace is NULL");
+  if (!aligned(workspace, 256)) return fail(CP_ERR_INVALID, who + "workspace must be 256-byte aligned");
+  if (workspace_bytes < need)
+    return fail(CP_ERR_CAPACITY, who + "workspace needs " + std::to_string(need) + " bytes");
+  const int rows = block_rows(max_q, p->G);
+  if (p->n_segments * ((max_q * p->G + rows - 1) / rows) > INT32_MAX / 2)
+    return fail(CP_ERR_UNSUPPORTED, who + "too many sequences of so many rows");
+  p->max_q = (int32_t)max_q;
+  p->n_shares = shares_of(rows);
+  p->narrow = cut(*p, rows);
+  unsigned char* const slots = static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares);
+  if (may_be_wide(rows, p->n_rows, p->Hq)) {
+    p->wide = cut(*p, kWideRows);
+    p->choice = reinterpret_cast<int32_t*>(slots - 256);
+  }
   p->starts = static_cast<ShareStart*>(workspace);
-  p->slots = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares));
+  p->slots = reinterpret_cast<float*>(slots);
   const std::string name = who.substr(0, who.size() - 2);
-  return p->block_rows == kChunkRows ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
+  return rows == kChunkRows ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
 }
 
 // The most rows of a sequence, from a batch's arguments.
@@ -108,7 +132,7 @@ extern "C" size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, i
     if (s != CP_OK) return s;
     s = check_rows(who, n_seqs, n_rows, false, &max_q, n_heads_q / n_heads_kv);
     if (s != CP_OK) return s;
-    if (n_rows > 0 && n_seqs > 0) total = workspace_bytes_of(max_q, n_heads_q / n_heads_kv);
+    if (n_rows > 0 && n_seqs > 0) total = workspace_bytes_of(n_rows, max_q, n_heads_q, n_heads_q / n_heads_kv);
     return CP_OK;
   });
   if (st != CP_OK) return 0;
@@ -153,7 +177,7 @@ extern "C" int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_str
     p.table_stride = kv->table_stride;
     p.table_len = (int32_t)std::min<int64_t>(INT32_MAX, kv->table_stride);
     p.paged_end = INT32_MAX;
-    p.key_end = (int32_t)std::min<int64_t>(kMaxTokens, kv->table_stride * kBlockTokens);
+    p.key_end = (int32_t)(std::min<int64_t>(kMaxTokens / kBlockTokens, kv->table_stride) * kBlockTokens);
     p.n_segments = kv->n_seqs;
     p.q_start = q_start;
     p.kv_len = kv->kv_len;
@@ -171,7 +195,7 @@ extern "C" size_t cp_attn_window_workspace_size(const cp_rank_plan* plan, int32_
     if (!plan) return fail(CP_ERR_INVALID, who + "plan is NULL");
     const int s = check_heads(n_heads_q, n_heads_kv, who);
     if (s != CP_OK) return s;
-    if (plan->n_rows > 0) total = workspace_bytes_of(plan->chunk_len, n_heads_q / n_heads_kv);
+    if (plan->n_rows > 0) total = workspace_bytes_of(plan->n_rows, plan->chunk_len, n_heads_q, n_heads_q / n_heads_kv);
     return CP_OK;
   });
   if (st != CP_OK) return 0;

@@ -63,7 +63,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
-  const Share share = find_share<kRowsThreads, kWaves, kSetup, 1, false>(p, blockIdx.x);
+  __shared__ int64_t wave_sum[kWaves];
+  const Blocks blocks = p.narrow;
+  const Counted counted = count_steps<kRowsThreads, kWaves, kSetup>(p, blocks, wave_sum);
+  const Share share = find_share<kWaves, kSetup, 1, false>(p, blocks, counted, blockIdx.x);
   if (tid == 0) p.starts[blockIdx.x] = share.at;
   if (same(share.at, share.end)) return;
 
@@ -79,7 +82,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   const ShareStart end = uniform(share.end);
   int place = __builtin_amdgcn_readfirstlane(share.at.place), kvh = __builtin_amdgcn_readfirstlane(share.at.kvh);
   int step = __builtin_amdgcn_readfirstlane(share.at.step);
-  Block x = block_at(p, place);
+  Block x = block_at(p, blocks, place);
   const Segment& s = x.s;
 
   // One part of a walk after another.  While the rows of one are combined and stored,
@@ -166,12 +169,12 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   for (bool first = true, more = true;; first = false) {
     Rows now = out;
     if (more) {
-      w = block_walk(p, s, x.block);
+      w = block_walk(p, blocks, s, x.block);
       const int n_steps = steps_of<kWaves>(w);
       const int stop = same_walk(end, ShareStart{place, kvh, 0, 0}) ? end.step : n_steps;
       now.o_row = s.o_row;
       now.rows = s.n * p.G;
-      now.r0 = x.block * p.block_rows;
+      now.r0 = x.block * (16 * NB);
       now.kvh = kvh;
       now.slot = step > 0 || stop < n_steps
                      ? p.slots + (2 * (size_t)blockIdx.x + (step > 0 ? 0 : 1)) * slot_floats(16 * NB)
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
     asm volatile("" ::: "memory");
 
     const bool last = same_walk(end, ShareStart{place, kvh, 0, 0});
-    more = !last && next_walk<false>(p, &x, &place, &kvh) && !same(end, ShareStart{place, kvh, 0, 0});
+    more = !last && next_walk<false>(p, blocks, &x, &place, &kvh) && !same(end, ShareStart{place, kvh, 0, 0});
     step = 0;
   }
 }
@@ -304,7 +307,7 @@ int launched(const char* who) {
 int launch_attn_rows(const PagedParams& p, void* stream, const char* who) {
   const dim3 grid((unsigned)p.n_shares), block(kRowsThreads);
   hipStream_t st = (hipStream_t)stream;
-  if (p.block_rows == 16)
+  if (p.narrow.rows == 16)
     hipLaunchKernelGGL(attn_rows_kernel<1>, grid, block, 0, st, p);
   else
     hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);

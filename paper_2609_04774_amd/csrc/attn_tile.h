@@ -135,17 +135,17 @@ __device__ __forceinline__ void open_tiles(const PagedParams& p, const Walk& w, 
 // Shares.  The walks of all blocks of rows are counted in steps of kTiles tiles and
 // cut into equal shares, one per workgroup.  Blocks are numbered as if every segment
 // had as many as the longest may have (the others have no rows and no steps), and
-// come in an order (PagedParams::run) that gives a workgroup, of a launch of several
+// come in an order (Blocks::run) that gives a workgroup, of a launch of several
 // blocks each, blocks far apart: those of neighbouring workgroups then pass over the
 // same keys at the same time.  The walks of a block's KV heads follow one another
 // (neighbouring workgroups read the same pages: what HBM serves best) or, with
 // kHeadsOuter, all blocks of a KV head do (the workgroups of an XCD share their keys in
 // its L2).
 
-__device__ __forceinline__ Walk block_walk(const PagedParams& p, const Segment& s, int block) {
-  const int r0 = block * p.block_rows;
+__device__ __forceinline__ Walk block_walk(const PagedParams& p, const Blocks& b, const Segment& s, int block) {
+  const int r0 = block * b.rows;
   const int rows = s.n * p.G;
-  return walk_of(p, s, r0, r0 + p.block_rows < rows ? r0 + p.block_rows : rows);
+  return walk_of(p, s, r0, r0 + b.rows < rows ? r0 + b.rows : rows);
 }
 
 // Steps of a walk; one at least, which stores the rows of a block without keys.
@@ -165,7 +165,7 @@ __device__ __forceinline__ ShareStart uniform(const ShareStart& x) {
 }
 
 // Places of the launch's order: run * stride, at least a place for each block.
-__device__ __forceinline__ int places(const PagedParams& p) { return p.run * p.stride; }
+__device__ __forceinline__ int places(const Blocks& b) { return b.run * b.stride; }
 
 struct Block {
   Segment s;
@@ -174,36 +174,36 @@ struct Block {
   int next;   // the first place after this one whose block may have rows
 };
 
-__device__ __forceinline__ Block block_at(const PagedParams& p, int place) {
+__device__ __forceinline__ Block block_at(const PagedParams& p, const Blocks& b, int place) {
   Block x;
-  const int i = p.run == 1 ? place : place % p.run * p.stride + place / p.run;
-  const int seg = p.blocks == 1 ? i : (int)((unsigned)i / (unsigned)p.blocks);
-  x.block = i - seg * p.blocks;
+  const int i = b.run == 1 ? place : place % b.run * b.stride + place / b.run;
+  const int seg = b.n == 1 ? i : (int)((unsigned)i / (unsigned)b.n);
+  x.block = i - seg * b.n;
   x.rows = false;
   x.next = place + 1;
   if (seg < p.n_segments) {
     x.s = segment_at(p, seg);
-    const int64_t left = (int64_t)x.s.n * p.G - (int64_t)x.block * p.block_rows;
+    const int64_t left = (int64_t)x.s.n * p.G - (int64_t)x.block * b.rows;
     x.rows = left > 0;
-    if (p.run == 1 && left <= p.block_rows) x.next = (seg + 1) * p.blocks;  // the segment's last one
+    if (b.run == 1 && left <= b.rows) x.next = (seg + 1) * b.n;  // the segment's last one
   }
   return x;
 }
 
 // The walk after this one, at its block; false behind the last.
 template <bool kHeadsOuter>
-__device__ __forceinline__ bool next_walk(const PagedParams& p, Block* x, int* place, int* kvh) {
+__device__ __forceinline__ bool next_walk(const PagedParams& p, const Blocks& b, Block* x, int* place, int* kvh) {
   if (!kHeadsOuter) {
     if (++*kvh < p.Hkv) return true;
     *kvh = 0;
   }
   do {
     *place = x->next;
-    if (*place >= places(p)) {
+    if (*place >= places(b)) {
       if (!kHeadsOuter || ++*kvh >= p.Hkv) return false;
       *place = 0;
     }
-    *x = block_at(p, *place);
+    *x = block_at(p, b, *place);
   } while (!x->rows);
   return true;
 }
@@ -214,7 +214,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return a / b;
 }
 
-// A share is [at, end); behind the last walk is place places(p).  A walk counts as its
+// A share is [at, end); behind the last walk is place places(b).  A walk counts as its
 // steps and kSetup more (its rows fetched, the first tiles waited for, the rows
 // stored).  A cut within those, or less than kSnap steps from the walk's start or end,
 // moves there: a shorter part costs more than it evens out.
@@ -222,57 +222,72 @@ struct Share {
   ShareStart at, end;
 };
 
-// Every thread counts the steps of its run of places, and a scan finds the walk of
-// each of the share's two ends.
-template <int kThreads, int kTiles, int kSetup, int kSnap, bool kHeadsOuter>
-__device__ Share find_share(const PagedParams& p, int share) {
-  __shared__ int64_t wave_sum[kThreads / 64];
-  __shared__ ShareStart found[2];
+// Every thread counts the steps of its run of places [i0, i1), `per` each, of one KV
+// head; `before` are those of the threads before it.
+struct Counted {
+  int64_t mine, before, total;
+  int i0, i1, per;
+};
+
+template <int kTiles, int kSetup>
+__device__ __forceinline__ int cost_of(const PagedParams& p, const Blocks& b, const Block& x) {
+  return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, b, x.s, x.block)) : 0;
+}
+
+template <int kThreads, int kTiles, int kSetup>
+__device__ Counted count_steps(const PagedParams& p, const Blocks& b, int64_t (&wave_sum)[kThreads / 64]) {
   const int tid = threadIdx.x;
-  const int n_places = places(p);
-  const int per = (n_places + kThreads - 1) / kThreads;
-  const int i0 = tid * per < n_places ? tid * per : n_places;
-  const int i1 = i0 + per < n_places ? i0 + per : n_places;
-  auto cost_of = [&](const Block& x) { return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, x.s, x.block)) : 0; };
-  int64_t mine = 0;
-  for (int i = i0; i < i1;) {
-    const Block x = block_at(p, i);
-    mine += cost_of(x);
+  const int n_places = places(b);
+  Counted c;
+  c.per = (n_places + kThreads - 1) / kThreads;
+  c.i0 = tid * c.per < n_places ? tid * c.per : n_places;
+  c.i1 = c.i0 + c.per < n_places ? c.i0 + c.per : n_places;
+  c.mine = 0;
+  for (int i = c.i0; i < c.i1;) {
+    const Block x = block_at(p, b, i);
+    c.mine += cost_of<kTiles, kSetup>(p, b, x);
     i = x.next;
   }
-  int64_t before = mine;
+  c.before = c.mine;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) {
-    const int64_t x = __shfl_up(before, k);
-    if ((tid & 63) >= k) before += x;
+    const int64_t x = __shfl_up(c.before, k);
+    if ((tid & 63) >= k) c.before += x;
   }
-  if ((tid & 63) == 63) wave_sum[tid >> 6] = before;
-  if (tid < 2) found[tid] = ShareStart{n_places, 0, 0, 0};
+  if ((tid & 63) == 63) wave_sum[tid >> 6] = c.before;
   __syncthreads();
-  int64_t total = 0;
+  c.total = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < (tid >> 6)) before += wave_sum[w];
-    total += wave_sum[w];
+    if (w < (tid >> 6)) c.before += wave_sum[w];
+    c.total += wave_sum[w];
   }
-  before -= mine;
-  const int64_t per_head = total > 0 ? total : 1;
-  total *= p.Hkv;
+  c.before -= c.mine;
+  return c;
+}
+
+// The thread whose places hold a share's end finds the walk there.
+template <int kTiles, int kSetup, int kSnap, bool kHeadsOuter>
+__device__ Share find_share(const PagedParams& p, const Blocks& b, const Counted& c, int share) {
+  __shared__ ShareStart found[2];
+  const int64_t per_head = c.total > 0 ? c.total : 1;
+  const int64_t total = c.total * p.Hkv;
   const int heads = kHeadsOuter ? 1 : p.Hkv;  // that share a step's place in the order
-  // With fewer steps than shares the last shares are empty.
+  // With fewer steps than shares the last shares are empty; of the others each end but
+  // the last is found by one thread.
   const int64_t n = total < p.n_shares ? total : p.n_shares;
   for (int e = 0; e < 2; ++e) {
     if (share + e >= n) continue;
     int64_t u = quotient(total * (share + e), n);
     const int head = kHeadsOuter ? (int)quotient(u, per_head) : 0;
-    u -= head * per_head + before * heads;
-    if (u < 0 || u >= mine * heads) continue;
-    for (int i = i0, next; i < i1; i = next) {
-      int cost = (int)mine;
+    u -= head * per_head + c.before * heads;
+    if (u < 0 || u >= c.mine * heads) continue;
+    for (int i = c.i0, next; i < c.i1; i = next) {
+      int cost = (int)c.mine;
       next = i + 1;
-      if (per > 1) {
-        const Block x = block_at(p, i);
-        cost = cost_of(x);
+      if (c.per > 1) {
+        const Block x = block_at(p, b, i);
+        cost = cost_of<kTiles, kSetup>(p, b, x);
         next = x.next;
       }
       if (u >= (int64_t)cost * heads) {
@@ -283,16 +298,17 @@ __device__ Share find_share(const PagedParams& p, int share) {
       int place = i, kvh = head + k, step = (int)(u - (int64_t)k * cost) - kSetup;
       if (step < kSnap) step = 0;
       if (step && cost - kSetup - step < kSnap) {
-        Block x = block_at(p, i);
+        Block x = block_at(p, b, i);
         step = 0;
-        if (!next_walk<kHeadsOuter>(p, &x, &place, &kvh)) place = n_places, kvh = 0;
+        if (!next_walk<kHeadsOuter>(p, b, &x, &place, &kvh)) place = places(b), kvh = 0;
       }
       found[e] = ShareStart{place, kvh, step, 0};
       break;
     }
   }
   __syncthreads();
-  return Share{found[0], found[1]};
+  const ShareStart behind = {places(b), 0, 0, 0};
+  return Share{share < n ? found[0] : behind, share + 1 < n ? found[1] : behind};
 }
 
 // ---------------------------------------------------------------------------

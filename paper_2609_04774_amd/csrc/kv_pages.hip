@@ -29,7 +29,7 @@ constexpr int kScanWaves = kScanThreads / 64;
 // first rows).
 template <int kLanes>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int64_t t = p.first_row + (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
   if (t >= p.n_rows) return;
   int s;
   int64_t end;
@@ -440,14 +440,19 @@ unsigned page_blocks(int64_t pages, int n) {
 
 }  // namespace
 
-int launch_append(const AppendParams& p, void* stream) {
+// A launch holds fewer than 2^32 threads: more rows take several.
+int launch_append(AppendParams p, void* stream) {
   const int64_t pieces = p.row_bytes >> 4;
   const int lanes = pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
-  const int64_t per_block = kThreads / lanes;
-  const dim3 grid((unsigned)((p.n_rows + per_block - 1) / per_block));
-  hipLaunchKernelGGL(lanes == 16 ? append_kernel<16> : lanes == 32 ? append_kernel<32> : append_kernel<64>, grid,
-                     dim3(kThreads), 0, (hipStream_t)stream, p);
-  return launched("cp_kv_append");
+  const int64_t per_block = kThreads / lanes, most = (int64_t)1 << 20;
+  for (; p.first_row < p.n_rows; p.first_row += most * per_block) {
+    const int64_t blocks = (p.n_rows - p.first_row + per_block - 1) / per_block;
+    hipLaunchKernelGGL(lanes == 16 ? append_kernel<16> : lanes == 32 ? append_kernel<32> : append_kernel<64>,
+                       dim3((unsigned)(blocks < most ? blocks : most)), dim3(kThreads), 0, (hipStream_t)stream, p);
+    const int st = launched("cp_kv_append");
+    if (st != CP_OK) return st;
+  }
+  return CP_OK;
 }
 
 int launch_copy_pages(const CacheSet& c, const int32_t* src, const int32_t* dst, int64_t n, void* stream) {

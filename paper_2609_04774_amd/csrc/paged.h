@@ -8,6 +8,13 @@ namespace cpattn {
 
 constexpr int kMaxTokens = 1 << 30;  // positions of one sequence
 
+// Blocks of rows (of one KV head) and their order.
+struct Blocks {
+  int32_t rows;         // of a block
+  int32_t n;            // blocks of a segment, at most
+  int32_t stride, run;  // place i of the order is block (i % run) * stride + i / run
+};
+
 // One launch of attention over a paged cache, of a batch's sequences (tables,
 // lengths and row starts in device memory) or of a rank's two chunks.
 struct PagedParams {
@@ -18,7 +25,7 @@ struct PagedParams {
   int64_t n_rows;          // rows of q (a batch's; at most 2^30)
   int32_t Hq, Hkv, G;      // G = Hq / Hkv
   int32_t window, n_sink;  // window 0: none
-  float scale, scale_log2;
+  float scale_log2;
 
   const unsigned char* k_cache;
   const unsigned char* v_cache;
@@ -48,9 +55,9 @@ struct PagedParams {
   // Workspace: where each workgroup's share of the walks begins, then two slots of
   // partial results per workgroup.
   int32_t n_shares;
-  int32_t block_rows;      // rows of a block (of one KV head)
-  int32_t blocks;          // of a segment, at most
-  int32_t stride, run;     // order of the blocks: place i is block (i % run) * stride + i / run
+  Blocks narrow;           // how the rows are cut into blocks,
+  Blocks wide;             // or in wide ones
+  int32_t* choice;         // of the two (1: wide), by the lengths; null: narrow
   struct ShareStart* starts;
   float* slots;
 };
@@ -63,7 +70,8 @@ struct ShareStart {
 
 constexpr int kRowsThreads = 256;
 constexpr int kChunkThreads = 512;
-constexpr int kChunkRows = 256;  // rows of a block of the kernel of many rows
+constexpr int kChunkRows = 256;    // rows of a block of the kernel of many rows,
+constexpr int kWideRows = 384;     // or of a long launch's
 constexpr int kRowsShares = 512;   // workgroups: two per compute unit
 constexpr int kChunkShares = 256;  // one
 
@@ -80,7 +88,7 @@ struct AppendParams {
   const unsigned char* k_rows;
   const unsigned char* v_rows;
   int64_t k_stride, v_stride;  // bytes between rows
-  int64_t n_rows;
+  int64_t first_row, n_rows;  // of this launch, and of all
   int64_t row_bytes;
   unsigned char* k_cache;
   unsigned char* v_cache;
@@ -92,7 +100,7 @@ struct AppendParams {
   int32_t n_seqs, uniform_q;
 };
 
-int launch_append(const AppendParams& p, void* stream);
+int launch_append(AppendParams p, void* stream);
 
 struct CacheSet {
   unsigned char* cache[CP_KV_MAX_CACHES];

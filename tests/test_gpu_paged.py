@@ -153,6 +153,45 @@ def test_a_long_chunk_among_many_sequences():
     b.check(*b.run(50, 4), 50, 4, rows=np.array([0, 1, 31, 32, 300, 699]))
 
 
+def wide(b, window=0, n_sink=0):
+    """A launch whose lengths choose wide blocks (the workspace says so behind the
+    256 shares' starts)."""
+    ws = torch.empty(cp.attn_paged_workspace_size(b.kv, len(b.q), b.max_q, b.Hq), dtype=torch.uint8, device=DEV)
+    out = b.run(window, n_sink, ws=ws)
+    assert ws.view(torch.int32)[1024] == 1
+    return out
+
+
+def test_wide_blocks():
+    b = Batch([17300, 40, 9000], [8192, 3, 129], 16, 1, seed=83)
+    rows = np.array([0, 1, 23, 24, 95, 96, 128, 383, 384, 1000, 4097, 8190, 8191])
+    first = wide(b)
+    b.check(*first, rows=rows)
+    again = wide(b)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    # A later token's infinite value shows in the rows that see it, in its column.  (The
+    # others keep their results within the bounds, not their bits: such a tile is taken
+    # by itself, and the weights around it against another maximum.)
+    at = 17300 - 4000
+    page, slot = int(b.tables[0, at // B]), at % B
+    b.vc[page, slot, 0, 7] = float("inf")
+    o, lse = wide(b)
+    i = 8192 - 4000
+    assert torch.equal(lse[8192:], first[1][8192:]) and torch.equal(o[8192:], first[0][8192:])
+    finite = torch.isfinite(o[:8192].float())
+    assert finite[:i].all() and not finite[i:, :, 7].any()
+    finite[:, :, 7] = True
+    assert finite.all()
+    b.v[0][at, 0, 7] = float("inf")
+    b.check(o, lse, rows=rows)
+
+
+def test_wide_blocks_window():
+    b = Batch([30000], [12288], 16, 1, seed=84)
+    b.hide(16384, 5)
+    b.check(*wide(b, 16384, 5), 16384, 5, rows=np.array([0, 95, 96, 1000, 5555, 12287]))
+
+
 def test_scale_and_strided_queries():
     b = Batch([77, 200, 9], [2, 2, 2], 8, 2, seed=77, uniform=True)
     o, lse = b.run(scale=0.3)
@@ -267,6 +306,19 @@ def test_append_positions(Hkv, head_dim):
                 wk[tables[s, pos // B], pos % B] = k[start[s] + i]
                 wv[tables[s, pos // B], pos % B] = v[start[s] + i]
     assert torch.equal(kc, wk) and torch.equal(vc, wv)
+
+
+def test_append_of_more_rows_than_a_launch_holds():
+    n = (1 << 24) + 1000  # narrow rows: 2^24 of a launch
+    pages = -(-n // B)
+    kc = torch.zeros(pages, B, 1, 8, dtype=torch.bfloat16, device=DEV)
+    vc = torch.zeros_like(kc)
+    tables = torch.arange(pages, dtype=torch.int32, device=DEV).flip(0).contiguous().view(1, pages)
+    kv = cp.PagedKV(kc, vc, tables, torch.tensor([n], dtype=torch.int32, device=DEV))
+    rows = (torch.arange(n * 8, dtype=torch.int32, device=DEV) % 30011).to(torch.int16).view(torch.bfloat16).view(n, 1, 8)
+    cp.kv_append(kv, rows, rows)
+    got = kc.flip(0).reshape(-1, 1, 8)[:n].view(torch.int16)
+    assert torch.equal(got, rows.view(torch.int16)) and torch.equal(vc.view(torch.int16), kc.view(torch.int16))
 
 
 def test_append_past_the_table_is_passed_over():

@@ -28,7 +28,7 @@ def paged(k=None, q=FAKE, q_stride=0, n_rows=2, q_start=FAKE, max_q=2, Hq=8, D=1
 
 @pytest.mark.parametrize("args,status", [
     (dict(k=kv(n_heads_kv=0)), INV), (dict(k=kv(n_heads_kv=3)), INV), (dict(Hq=0), INV), (dict(Hq=8192), UNS),
-    (dict(D=64), UNS), (dict(scale=float("nan")), INV), (dict(scale=float("inf")), INV), (dict(window=-1), INV),
+    (dict(D=64), UNS), (dict(scale=float("nan")), INV), (dict(scale=float("inf")), INV), (dict(window=-1), INV), (dict(scale=3e38), INV),
     (dict(n_sink=-1), INV), (dict(n_rows=-1), INV), (dict(k=kv(n_seqs=-1)), INV), (dict(n_rows=(1 << 30) + 1), UNS),
     (dict(n_rows=1 << 30, Hq=64), UNS), (dict(q_start=None, n_rows=3), INV), (dict(max_q=0), INV),
     (dict(q_stride=512), INV), (dict(q_stride=1028), INV), (dict(q_stride=-1024), INV), (dict(k=kv(n_blocks=-1)), INV),
@@ -58,6 +58,7 @@ def test_workspace_sizes():
     one = size(2, 2, 1, 8, 2)
     assert 0 < one <= size(2, 64, 32, 8, 2)
     assert paged(q_start=None, n_rows=2, ws_bytes=one - 1) == CAP and str(one) in cp.last_error()
+    assert size(2, 64, 64, 8, 2) <= size(2, 1 << 16, 64, 8, 2)  # rows that may be cut into wide blocks
     plan, _ = cp.shard_plan(0, 100, 2, 0)
     assert cp.attn_window_workspace_size(plan, 8, 2) > 0
     with pytest.raises(cp.CpError):
