@@ -196,9 +196,23 @@ template <class List, bool kFork>
 __global__ __launch_bounds__(kScanThreads) void take_pages_kernel(cp_kv_pool p, List list, int n, int32_t* missing) {
   __shared__ __attribute__((aligned(16))) int32_t seqs[CP_KV_MAX_LIST], second[kFork ? CP_KV_MAX_LIST : 4];
   __shared__ int64_t need_end[CP_KV_MAX_LIST];  // pages that the entries up to this one want
+  __shared__ int32_t first_of[CP_KV_MAX_LIST];  // table entry of an entry's first page
   __shared__ int64_t wave_sum[kScanWaves];
   __shared__ int32_t n_missing;
   const int tid = threadIdx.x;
+  // Which of kEach pages from `at` on are free.  The first are looked up at once, while
+  // the lists are read.
+  constexpr int kEach = 8;
+  auto free_from = [&](int64_t at) {
+    int32_t refs[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) refs[j] = at + j < p.n_blocks ? p.refs[at + j] : 1;
+    uint32_t free = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) free |= (uint32_t)(refs[j] == 0) << j;
+    return free;
+  };
+  uint32_t free = free_from((int64_t)tid * kEach);
   for (int i = tid; i < n; i += kScanThreads) {
     seqs[i] = list.seqs[i];
     if constexpr (kFork) second[i] = list.parents[i];
@@ -234,18 +248,15 @@ __global__ __launch_bounds__(kScanThreads) void take_pages_kernel(cp_kv_pool p, 
     if (k >= per || i >= n) continue;
     end += w[k].n;
     need_end[i] = end;
+    first_of[i] = (int32_t)w[k].first;
   }
   __syncthreads();
   // Pages of rank 0 .. total - 1 among the free ones, each into its entry.
   const int64_t total = s.total;
   int64_t found = 0;
-  constexpr int kEach = 8;
   for (int64_t base = 0; base < p.n_blocks && found < total; base += (int64_t)kScanThreads * kEach) {
     const int64_t at = base + (int64_t)tid * kEach;
-    uint32_t free = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j)
-      if (at + j < p.n_blocks && p.refs[at + j] == 0) free |= 1u << j;
+    if (base > 0) free = free_from(at);
     const Scan f = scan(__builtin_popcount(free), wave_sum);
     int64_t rank = found + f.before;
     while (free && rank < total) {
@@ -261,13 +272,7 @@ __global__ __launch_bounds__(kScanThreads) void take_pages_kernel(cp_kv_pool p, 
       }
       // Its first page's rank is the end of the entry before.
       const int64_t k = rank - (lo ? need_end[lo - 1] : 0);
-      const int seq = seqs[lo];
-      int64_t first;
-      if constexpr (kFork)
-        first = clamp_len(p.kv_len[second[lo]]) / kBlockTokens;
-      else
-        first = pages_of(clamp_len(p.kv_len[seq]));
-      p.tables[seq * p.table_stride + first + k] = (int32_t)page;
+      p.tables[seqs[lo] * p.table_stride + first_of[lo] + k] = (int32_t)page;
       p.refs[page] = 1;
       ++rank;
     }
