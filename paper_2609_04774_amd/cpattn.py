@@ -13,6 +13,8 @@ import math
 import os
 from typing import Optional, Sequence
 
+import torch  # before the library: see _load
+
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG_DIR, "libcpattn.so")
 
@@ -101,7 +103,6 @@ def _load():
     # torch ships its own HIP runtime (same soname).  Loading torch first makes
     # libcpattn bind to that already-loaded runtime, so the process has one
     # HIP runtime and torch's streams and allocations are valid in the library.
-    import torch  # noqa: F401
     lib = ctypes.CDLL(LIB_PATH)
     lib.cp_status_string.restype = ctypes.c_char_p
     lib.cp_status_string.argtypes = [ctypes.c_int]
@@ -502,30 +503,32 @@ def repartition_all(prefix_len: int, new_len: int, src_sets, dst_sets, stream=No
 
 # --- attention over a paged cache -----------------------------------------------------
 
-def _same_device(device, named, stream=None):
-    """The calls below launch on the current device: every tensor, and the
-    stream if one is given, has to be there."""
-    import torch
+def _stream_on(device: int, named, stream) -> Optional[int]:
+    """The stream's handle.  The calls below launch on the current device: every
+    tensor, and the stream if one is given, has to be there."""
     here = torch.cuda.current_device()
-    if device.index != here:
-        raise ValueError(f"the tensors are on {device}, the current device is cuda:{here}")
+    if device != here:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{here}")
     for name, t in named:
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if stream is not None and stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, expected {device}")
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} is on {t.device}, expected cuda:{device}")
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # as _stream_handle
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(device)
+    if stream.device.index != device:
+        raise ValueError(f"the stream is on {stream.device}, expected cuda:{device}")
+    return stream.cuda_stream
 
 
 def _rows_of(t, name: str, heads: int, D: int):
     """Elements between the rows of a bf16 GPU tensor [rows, heads, D] whose
     rows are dense (a slice of a fused projection's output is fine)."""
-    import torch
+    shape, stride = t.shape, t.stride()
     if t.dtype != torch.bfloat16 or not t.is_cuda:
         _dev(t, name, torch.bfloat16)
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
-        raise ValueError(f"{name} must have shape [rows, {heads}, {D}], has {tuple(t.shape)}")
-    rows, _, _ = t.shape
-    stride = t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != D:
+        raise ValueError(f"{name} must have shape [rows, {heads}, {D}], has {tuple(shape)}")
+    rows = shape[0]
     if rows and ((heads > 1 and stride[1] != D) or (D > 1 and stride[2] != 1) or
                  (rows > 1 and (stride[0] < heads * D or stride[0] % 8))):
         raise ValueError(f"the rows of {name} must be dense, and a multiple of 8 elements apart")
@@ -539,7 +542,6 @@ class PagedKV:
     contents may change between calls."""
 
     def __init__(self, k_cache, v_cache, tables, kv_len):
-        import torch
         for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
             _dev(t, name, torch.bfloat16)
             if t.dim() != 4 or t.shape[1] != CP_KV_BLOCK_TOKENS:
@@ -562,9 +564,8 @@ class PagedKV:
                                 _ptr(kv_len), self.n_seqs, self.n_heads)
         self.ref = ctypes.byref(self.struct)
 
-    def check_rows(self, n_rows: int, q_start):
+    def check_starts(self, q_start):
         """q_start's checks; its address."""
-        import torch
         if q_start is None:
             return None
         if q_start.dtype != torch.int32 or q_start.dim() != 1 or q_start.shape[0] != self.n_seqs + 1:
@@ -582,7 +583,6 @@ def attn_paged_workspace_size(kv: PagedKV, n_rows: int, max_q: int, n_heads_q: i
 
 
 def _check_out(o, lse, rows: int, heads: int, D: int):
-    import torch
     if o.dtype != torch.bfloat16 or not o.is_cuda or not o.is_contiguous() or o.dim() != 3 or o.shape[0] < rows \
             or o.shape[1] != heads or o.shape[2] != D:
         _dev(o, "o", torch.bfloat16, rows, (heads, D))
@@ -600,15 +600,16 @@ def attn_paged(kv: PagedKV, q, o, workspace, lse=None, q_start=None, max_q: Opti
     uint8 GPU tensor of attn_paged_workspace_size bytes."""
     rows, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
     stride = _rows_of(q, "q", Hq, kv.head_dim)
-    start = kv.check_rows(rows, q_start)
+    start = kv.check_starts(q_start)
     if start is not None and max_q is None:
         raise ValueError("max_q is needed with q_start")
     _check_out(o, lse, rows, Hq, kv.head_dim)
     _dev(workspace, "workspace")
-    _same_device(kv.device, (("q", q), ("o", o), ("lse", lse), ("q_start", q_start), ("workspace", workspace)), stream)
+    handle = _stream_on(kv.device.index, (("q", q), ("o", o), ("lse", lse), ("q_start", q_start),
+                                          ("workspace", workspace)), stream)
     _check(lib.cp_attn_paged(kv.ref, q.data_ptr(), stride, rows, start, max_q or 0, Hq, kv.head_dim, softmax_scale,
                              window, n_sink, o.data_ptr(), _ptr(lse), workspace.data_ptr(),
-                             workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+                             workspace.numel() * workspace.element_size(), handle))
 
 
 def attn_window_workspace_size(plan: CpRankPlan, n_heads_q: int, n_heads_kv: int) -> int:
@@ -626,7 +627,6 @@ def attn_window(plan: CpRankPlan, q, k_new, v_new, o, workspace, window: int, n_
     (caches [blocks, 16, Hkv, 128], needed when the plan has one) and k_new,
     v_new bf16 [R, Hkv, 128].  o bf16 (and lse float32) has the rank's rows, or
     R rows with out_order=CP_OUT_SEQUENCE."""
-    import torch
     D = CP_HEAD_DIM
     if q.dim() != 3 or k_new.dim() != 3:
         raise ValueError("q and k_new must have shape [rows, heads, 128]")
@@ -649,12 +649,13 @@ def attn_window(plan: CpRankPlan, q, k_new, v_new, o, workspace, window: int, n_
     else:
         k_cache = v_cache = block_table = None
     _dev(workspace, "workspace")
-    _same_device(q.device, (("k_new", k_new), ("v_new", v_new), ("o", o), ("lse", lse), ("k_cache", k_cache),
-                            ("v_cache", v_cache), ("block_table", block_table), ("workspace", workspace)), stream)
+    handle = _stream_on(q.device.index, (("k_new", k_new), ("v_new", v_new), ("o", o), ("lse", lse),
+                                         ("k_cache", k_cache), ("v_cache", v_cache), ("block_table", block_table),
+                                         ("workspace", workspace)), stream)
     _check(lib.cp_attn_window(ctypes.byref(plan), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache),
                               n_blocks, _ptr(block_table), table_len, Hq, Hkv, D, softmax_scale, window, n_sink,
                               _ptr(o), _ptr(lse), out_order, _ptr(workspace),
-                              workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+                              workspace.numel() * workspace.element_size(), handle))
 
 
 # --- pages of a cache -------------------------------------------------------------------
@@ -668,10 +669,10 @@ def kv_append(kv: PagedKV, k_rows, v_rows, q_start=None, stream=None):
     rows = k_rows.shape[0]
     if v_rows.shape[0] != rows:
         raise ValueError("k_rows and v_rows differ in rows")
-    start = kv.check_rows(rows, q_start)
-    _same_device(kv.device, (("k_rows", k_rows), ("v_rows", v_rows), ("q_start", q_start)), stream)
+    start = kv.check_starts(q_start)
+    handle = _stream_on(kv.device.index, (("k_rows", k_rows), ("v_rows", v_rows), ("q_start", q_start)), stream)
     _check(lib.cp_kv_append(kv.ref, k_rows.data_ptr(), v_rows.data_ptr(), k_stride, v_stride, rows, start, kv.head_dim,
-                            _stream_handle(stream)))
+                            handle))
 
 
 class _Caches:
@@ -699,7 +700,6 @@ class KVPool:
     buffers that an engine keeps."""
 
     def __init__(self, tables, kv_len, refs, caches=()):
-        import torch
         _dev(tables, "tables", torch.int32)
         if tables.dim() != 2:
             raise ValueError("tables must have shape [n_seqs, pages]")
@@ -719,9 +719,9 @@ class KVPool:
                                tables.shape[0], 0)
         self.ref = ctypes.byref(self.struct)
 
-    def check_lists(self, stream, missing=None, **lists) -> int:
-        """The lists' common length: int32 tensors of one dimension on the pool's device."""
-        import torch
+    def check_lists(self, stream, missing=None, **lists):
+        """The lists' common length and the stream's handle; they are int32 tensors
+        of one dimension on the pool's device."""
         n = None
         for name, t in lists.items():
             if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
@@ -733,14 +733,12 @@ class KVPool:
         if missing is not None:
             _dev(missing, "missing", torch.int32, 1)
             lists["missing"] = missing
-        _same_device(self.device, lists.items(), stream)
-        return n
+        return n, _stream_on(self.device.index, lists.items(), stream)
 
 
 def kv_copy_pages(caches, src, dst, stream=None):
     """cp_kv_copy_pages: page src[i] to page dst[i] (int32 GPU tensors) in every
     one of ``caches`` (tensors [blocks, ...], or a KVPool's)."""
-    import torch
     c = caches.caches if isinstance(caches, KVPool) else _Caches(tuple(caches))
     if c.n == 0:
         raise ValueError("at least one cache")
@@ -748,31 +746,31 @@ def kv_copy_pages(caches, src, dst, stream=None):
         _dev(t, name, torch.int32)
     if src.dim() != 1 or dst.shape != src.shape:
         raise ValueError("src and dst must have one dimension and one length")
-    _same_device(c.tensors[0].device, (("src", src), ("dst", dst)), stream)
+    handle = _stream_on(c.tensors[0].device.index, (("src", src), ("dst", dst)), stream)
     _check(lib.cp_kv_copy_pages(c.ptrs, c.n, c.n_blocks, c.page_bytes, _ptr(src), _ptr(dst), src.shape[0],
-                                _stream_handle(stream)))
+                                handle))
 
 
 def kv_reserve(pool: KVPool, seqs, add, missing, stream=None):
     """cp_kv_reserve: room for add[i] more tokens of sequence seqs[i]; missing
     int32 [1] receives how many entries got none."""
-    n = pool.check_lists(stream, missing, seqs=seqs, add=add)
-    _check(lib.cp_kv_reserve(pool.ref, _ptr(seqs), _ptr(add), n, _ptr(missing), _stream_handle(stream)))
+    n, handle = pool.check_lists(stream, missing, seqs=seqs, add=add)
+    _check(lib.cp_kv_reserve(pool.ref, _ptr(seqs), _ptr(add), n, _ptr(missing), handle))
 
 
 def kv_fork(pool: KVPool, parents, children, missing, stream=None):
     """cp_kv_fork: sequence children[i] continues parents[i], sharing its full
     pages; a page filled in part is copied in every cache of the pool."""
-    n = pool.check_lists(stream, missing, parents=parents, children=children)
+    n, handle = pool.check_lists(stream, missing, parents=parents, children=children)
     c = pool.caches
     _check(lib.cp_kv_fork(pool.ref, c.ptrs, c.n, c.page_bytes, _ptr(parents), _ptr(children), n, _ptr(missing),
-                          _stream_handle(stream)))
+                          handle))
 
 
 def kv_free(pool: KVPool, seqs, begin, end, stream=None):
     """cp_kv_free: the pages of sequence seqs[i] whose tokens lie in [begin[i], end[i])."""
-    n = pool.check_lists(stream, seqs=seqs, begin=begin, end=end)
-    _check(lib.cp_kv_free(pool.ref, _ptr(seqs), _ptr(begin), _ptr(end), n, _stream_handle(stream)))
+    n, handle = pool.check_lists(stream, seqs=seqs, begin=begin, end=end)
+    _check(lib.cp_kv_free(pool.ref, _ptr(seqs), _ptr(begin), _ptr(end), n, handle))
 
 
 def kv_compact_workspace_size(pool: KVPool) -> int:
@@ -783,7 +781,7 @@ def kv_compact_workspace_size(pool: KVPool) -> int:
 def kv_compact(pool: KVPool, workspace, stream=None):
     """cp_kv_compact: the pool's pages in use to its front, tables and counts with them."""
     _dev(workspace, "workspace")
-    _same_device(pool.device, (("workspace", workspace),), stream)
+    handle = _stream_on(pool.device.index, (("workspace", workspace),), stream)
     c = pool.caches
     _check(lib.cp_kv_compact(pool.ref, c.ptrs, c.n, c.page_bytes, _ptr(workspace),
-                             workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+                             workspace.numel() * workspace.element_size(), handle))
