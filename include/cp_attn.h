@@ -453,8 +453,9 @@ typedef struct cp_paged_kv {
 
 /*
  * Sizing call of cp_attn_paged (a library utility, not from the paper): device
- * bytes of its workspace for any contents of the device arrays; 0 on invalid
- * arguments (cp_last_error says why).
+ * bytes of its workspace for any contents of the device arrays, and for calls of
+ * fewer rows; 0 on invalid arguments (cp_last_error says why).  max_q is the
+ * call's, without q_start n_rows / n_seqs.
  */
 size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_q, int32_t n_heads_q,
                                     int32_t n_heads_kv);
@@ -473,7 +474,7 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  *               a sequence past it are left as they were.  Up to 32 (row, query
  *               head) pairs per KV head take a kernel for few rows.
  *   n_heads_q   a multiple of n_heads_kv; head_dim 128.
- *   softmax_scale  <= 0 selects 1/sqrt(head_dim).
+ *   softmax_scale  <= 0 selects 1/sqrt(head_dim); below 2^127 otherwise.
  *   window      keys visible behind a row, itself included; 0: all.
  *   n_sink      first positions that stay visible behind the window, >= 0.
  *   o           bf16 [n_rows][n_heads_q][128].
@@ -484,9 +485,10 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  * A row that sees no key has O = 0, LSE = -inf; a NaN among its scores gives O =
  * NaN, LSE = -inf.  Keys and values that a row does not see have no effect on
  * it, whatever they hold.
- * Errors: CP_ERR_INVALID (shapes, pointers, alignment, window or n_sink < 0),
+ * Errors: CP_ERR_INVALID (shapes, pointers, alignment, scale, window or n_sink < 0),
  * CP_ERR_UNSUPPORTED (head_dim; n_rows above 2^30, or times n_heads_q /
- * n_heads_kv above 2^31 - 1), CP_ERR_CAPACITY (workspace), CP_ERR_HIP.
+ * n_heads_kv above 2^31 - 1; n_seqs times max_q rows beyond 2^30 blocks),
+ * CP_ERR_CAPACITY (workspace), CP_ERR_HIP.
  */
 int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_stride, int64_t n_rows, const int32_t* q_start,
                   int64_t max_q, int32_t n_heads_q, int32_t head_dim, float softmax_scale, int64_t window,

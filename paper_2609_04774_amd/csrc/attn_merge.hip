@@ -16,8 +16,10 @@ using namespace tile;
 // it.  Block (x, y): the walk that share x + 1 begins within, if it is the first to do
 // so; a wave takes kRows rows.
 //
-// Bound by latency: what tells the walk and its parts is read at once, and eight
-// parts' rows are in flight.
+// Bound by latency for blocks of few rows: what tells the walk and its parts is read at
+// once, and eight parts' rows are in flight (6 us, 64 parts or two; with the parts
+// dealt to four waves, and the rows fetched along with their LSEs, 6 to 9).  Else by the
+// parts' bytes: 384 rows of 255 walks, 150 MB, 32 us.
 template <int kRows>
 __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
   constexpr int kParts = 8 / kRows;

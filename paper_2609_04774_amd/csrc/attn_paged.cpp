@@ -51,7 +51,7 @@ int shares_of(int block_rows) { return block_rows == kChunkRows ? kChunkShares :
 
 // Whether wide blocks (the lengths decide on them) are worth a second kernel's launch, 4 us
 // where it has nothing to do.  One prompt's 4096 rows of 32 and 8 heads with and without
-// the choice: alone 176 and 173 us, after 8K tokens 608 and 642, after 32K 1875 and 2049;
+// the choice: alone 203 and 204 us, after 8K tokens 654 and 684, after 32K 1839 and 1961;
 // 2048 rows alone 84 and 80, after 8K 315 and 316, after 32K 978 and 1016.
 bool may_be_wide(int block_rows, int64_t n_rows, int32_t Hq) {
   return block_rows == kChunkRows && n_rows * Hq >= 131072;

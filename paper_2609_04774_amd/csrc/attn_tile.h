@@ -1,4 +1,4 @@
-// Building blocks of the attention kernels over a paged cache (attn_paged.hip,
+// Building blocks of the attention kernels over a paged cache (attn_rows.hip,
 // attn_chunk.hip): where a segment's keys lie, which of them a block of rows
 // walks, and 32-key tiles of K and V in LDS as operands of the matrix cores.
 #pragma once
