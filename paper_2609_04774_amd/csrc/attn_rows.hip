@@ -22,7 +22,7 @@
 //
 // Measured (32 query and 8 KV heads): 64 sequences of 8192 keys 370 us, 5.8 TB/s, where
 // a plain read of as much runs at 6.0 to 6.5; of 200 to 32768 keys 264 us, 5.1 TB/s with
-// the shares' starts (8 us) and the merge (6).  One sequence of 4101 keys 19 us, of which
+// the merge (6 us).  One sequence of 4101 keys 19 us, of which
 // the merge is 6: latency (the lengths, the pages, the keys, one after another).
 // Four or eight waves with a head each, as many shares again, or shares numbered by XCD
 // were no faster.  With this kernel's work left to that of many rows the same batches

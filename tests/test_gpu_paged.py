@@ -192,6 +192,39 @@ def test_wide_blocks_window():
     b.check(*wide(b, 16384, 5), 16384, 5, rows=np.array([0, 95, 96, 1000, 5555, 12287]))
 
 
+def test_captured_launch_follows_the_choice_of_blocks():
+    """Replays of one capture whose lengths ask for wide blocks, for narrow ones, and
+    for wide ones again, against the oracle and the eager call."""
+    b = Batch([17300], [8192], 16, 1, seed=85)
+    rows = np.array([0, 95, 96, 255, 256, 4097, 8191])
+    q = b.q.to(DEV)
+    o, lse = torch.empty_like(q), torch.empty(8192, 16, device=DEV)
+    ws = torch.empty(cp.attn_paged_workspace_size(b.kv, 8192, 8192, 16), dtype=torch.uint8, device=DEV)
+
+    def step():
+        cp.attn_paged(b.kv, q, o, ws, lse=lse, q_start=b.q_start, max_q=8192)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for length, choice in ((17300, 1), (8192, 0), (5000, 0), (17300, 1)):
+        b.kv_len[0] = length
+        b.dev_len.fill_(length)
+        o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(ws.view(torch.int32)[1024]) == choice
+        got = o.clone(), lse.clone()
+        k, v = b.k[0], b.v[0]
+        b.k[0], b.v[0] = k[:length], v[:length]
+        b.check(*got, rows=rows)
+        b.k[0], b.v[0] = k, v
+        step()
+        assert torch.equal(o, got[0]) and torch.equal(lse, got[1])
+
+
 def test_scale_and_strided_queries():
     b = Batch([77, 200, 9], [2, 2, 2], 8, 2, seed=77, uniform=True)
     o, lse = b.run(scale=0.3)
