@@ -108,5 +108,5 @@ def compare(o, lse, want, n_keys, what):
     assert np.nanmax(err, initial=0.0) <= 1.0, f"{what}: O off by {np.nanmax(err):.3g} of its bound"
     if lse is not None:
         assert np.array_equal(np.isneginf(lse), empty), f"{what}: LSE of empty rows"
-        err = np.abs(lse - wl)[~empty] / on_lse[~empty]
+        err = np.abs(lse[~empty] - wl[~empty]) / on_lse[~empty]
         assert err.max(initial=0.0) <= 1.0, f"{what}: LSE off by {err.max():.3g} of its bound"

@@ -77,6 +77,12 @@ def test_long_window():
     run(4096, 4100, 2, 8, 1, 3000, 9, seed=10, rows_checked=np.array([0, 1, 500, 1023, 1024, 1025, 2040, 2049]))
 
 
+def test_many_rows_in_sequence_order():
+    """Enough rows for wide blocks, over the prefix and the new tokens."""
+    run(4800, 16384, 2, 16, 1, 0, 0, seed=14, order=cp.CP_OUT_SEQUENCE,
+        rows_checked=np.array([0, 95, 96, 255, 256, 4095, 4096, 8191]))
+
+
 def test_pages_that_name_nothing():
     def edit(k, v, kc, vc, table):
         table[2], table[4] = -1, len(kc)
