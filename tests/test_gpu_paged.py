@@ -315,6 +315,46 @@ def test_another_stream():
 
 # --- append ------------------------------------------------------------------------------
 
+def test_two_calls_at_once():
+    """Calls on two streams, each with its workspace, and a page copy beside them."""
+    a = Batch([3000, 50, 900], [1, 1, 1], 8, 2, seed=86, uniform=True)
+    b = Batch([700, 300], [200, 64], 8, 2, seed=87)
+    want = a.run(), b.run()
+    torch.cuda.synchronize()
+    sides = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [[], []]
+    for _ in range(8):
+        for side, batch, out in zip(sides, (a, b), got):
+            with torch.cuda.stream(side):
+                out.append(batch.run())
+    torch.cuda.synchronize()
+    for out, w in zip(got, want):
+        assert all(torch.equal(o, w[0]) and torch.equal(l, w[1]) for o, l in out)
+
+
+@pytest.mark.parametrize("new", [2, 90])
+def test_offsets_beyond_32_bits(new):
+    """Pages at the end of caches of 4.6 GB."""
+    b = Batch([333, 40], [new, 3], 32, 8, seed=88)
+    n = 140000
+    kc = torch.empty(n, B, 8, D, dtype=torch.bfloat16, device=DEV)
+    vc = torch.empty_like(kc)
+    tables = torch.where(b.tables >= 0, n - 1 - b.tables, b.tables).to(DEV)
+    kv = cp.PagedKV(kc, vc, tables, b.dev_len)
+    starts = torch.tensor([0, 333, 373], dtype=torch.int32, device=DEV)
+    cp.kv_append(kv, torch.cat(b.k).to(DEV), torch.cat(b.v).to(DEV), q_start=starts)
+    o, lse = torch.empty(new + 3, 32, D, dtype=torch.bfloat16, device=DEV), torch.empty(new + 3, 32, device=DEV)
+    ws = torch.empty(cp.attn_paged_workspace_size(kv, new + 3, max(new, 3), 32), dtype=torch.uint8, device=DEV)
+    for window in (0, 60):
+        cp.attn_paged(kv, b.q.to(DEV), o, ws, lse=lse, q_start=b.q_start, max_q=max(new, 3), window=window, n_sink=2)
+        b.check(o, lse, window, 2, rows=np.arange(0, 90, 7))
+    pages = tables[tables >= 0].flip(0).contiguous()
+    low = torch.arange(len(pages), dtype=torch.int32, device=DEV)
+    cp.kv_copy_pages([kc, vc], pages, low)
+    for c in (kc, vc):
+        assert torch.equal(c[:len(pages)].view(torch.int16), c[pages.long()].view(torch.int16))
+
+
 @pytest.mark.parametrize("Hkv,head_dim", [(1, 128), (2, 128), (8, 128), (3, 40)])
 def test_append_positions(Hkv, head_dim):
     """Ragged rows at odd positions, from a strided source; every other slot, and

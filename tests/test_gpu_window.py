@@ -124,6 +124,24 @@ def test_later_values_do_not_reach_earlier_rows():
     assert np.abs(got - want)[~hit].max() <= 2.0**-7 * np.abs(want).max()
 
 
+def test_prefix_offsets_beyond_32_bits():
+    P, R = 64, 70
+    g = torch.Generator().manual_seed(15)
+    q, k, v, pk, pv = (randn(g, n, h, D) for n, h in ((R, 32), (R, 8), (R, 8), (P, 8), (P, 8)))
+    kc = torch.empty(140000, B, 8, D, dtype=torch.bfloat16, device=DEV)  # 4.6 GB
+    vc = torch.empty_like(kc)
+    table = torch.tensor([139999, 139000, 5, 139500], dtype=torch.int32, device=DEV)
+    kc[table.long()], vc[table.long()] = pk.view(4, B, 8, D).to(DEV), pv.view(4, B, 8, D).to(DEV)
+    plan, rows = cp.shard_plan(P, R, 1, 0)
+    o, lse = torch.empty(R, 32, D, dtype=torch.bfloat16, device=DEV), torch.empty(R, 32, device=DEV)
+    ws = torch.empty(cp.attn_window_workspace_size(plan, 32, 8), dtype=torch.uint8, device=DEV)
+    cp.attn_window(plan, q.to(DEV), k.to(DEV), v.to(DEV), o, ws, 50, n_sink=3, lse=lse, k_cache=kc, v_cache=vc,
+                   block_table=table)
+    want = owin.attend(f64(q), rows, np.concatenate([f64(pk), f64(k)]), np.concatenate([f64(pv), f64(v)]),
+                       np.arange(P + R), 50, 3)
+    compare(f64(o), f64(lse), want, P + R, "rows")
+
+
 def test_plan_without_rows():
     plan, _ = cp.shard_plan(0, 3, 8, 5)
     assert plan.n_rows == 0
