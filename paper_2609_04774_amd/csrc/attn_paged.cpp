@@ -12,6 +12,8 @@ using namespace cpattn;
 
 namespace {
 
+constexpr int64_t kInfinityCacheBytes = 256 << 20;
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 int check_heads(int32_t Hq, int32_t Hkv, const std::string& who) {
@@ -176,6 +178,7 @@ extern "C" int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_str
     p.tables = kv->tables;
     p.table_stride = kv->table_stride;
     p.table_len = (int32_t)std::min<int64_t>(INT32_MAX, kv->table_stride);
+    p.streamed = 2 * kv->n_blocks > kInfinityCacheBytes / (kBlockTokens * p.kv_stride);
     p.paged_end = INT32_MAX;
     p.key_end = (int32_t)(std::min<int64_t>(kMaxTokens / kBlockTokens, kv->table_stride) * kBlockTokens);
     p.n_segments = kv->n_seqs;

@@ -20,13 +20,18 @@
 // meet only at the end of a walk; the eight waves of a compute unit keep about 128
 // KB in flight.
 //
-// Measured (32 query and 8 KV heads): 64 sequences of 8192 keys 370 us, 5.8 TB/s, where
-// a plain read of as much runs at 6.0 to 6.5; of 200 to 32768 keys 264 us, 5.1 TB/s with
-// the merge (6 us).  One sequence of 4101 keys 19 us, of which
+// Long walks over a pool that the Infinity Cache (256 MB) cannot hold stream (loads with
+// the non-temporal hint), but for pages that another sequence of the batch names too
+// (a shared prefix).  64 sequences of 8192 keys 338 us against 370 with plain loads; of
+// one prefix of 8192 keys 117, of 32768 keys for 32 sequences 225 (streamed, 346).  Walks of
+// fewer keys than 1280 do not: at 300 they take 246 us plain and 278 streamed, at 1024
+// 229 and 233, at 1536 226 and 222, at 4096 230 and 215 (1.2 GB each).
+//
+// Measured (32 query and 8 KV heads): 64 sequences of 8192 keys 338 us, 6.35 TB/s, where
+// a plain read of as much runs at 6.0 to 6.5.  One sequence of 4101 keys 19 us, of which
 // the merge is 6: latency (the lengths, the pages, the keys, one after another).
 // Four or eight waves with a head each, as many shares again, or shares numbered by XCD
-// were no faster.  With this kernel's work left to that of many rows the same batches
-// take 5 to 10 % more.
+// were no faster.
 #include <hip/hip_runtime.h>
 
 #include "attn_tile.h"
@@ -40,12 +45,14 @@ using namespace tile;
 constexpr int kWaves = kRowsThreads / 64;
 constexpr int kWaveBytes = 2 * kTileBytes;  // a tile of K and one of V
 constexpr int kSetup = 1;                   // of a walk, in steps
+constexpr int kStreamTiles = 40;            // of a walk whose loads stream
 constexpr int kLoads = kTileBytes / 1024;   // direct-to-LDS loads of a tile and tensor, 1 KB each
 
 // One tile's loads of K (tensor 0) or V: 1 KB each, four keys of 256 bytes.  `off`
-// are this lane's offsets within a half (four loads of it).
+// are this lane's offsets within a half (four loads of it).  Bit `half` of kept: with
+// plain loads, else with streaming ones.
 __device__ __forceinline__ void load_tile(const PagedParams& p, const Walk& w, int t0, int kvh, int pages, int first,
-                                          const uint32_t (&off)[4], int lane, uint32_t dst, int tensor) {
+                                          uint64_t kept, const uint32_t (&off)[4], int lane, uint32_t dst, int tensor) {
   const unsigned char* cache = tensor ? p.v_cache : p.k_cache;
   const unsigned char* fresh = tensor ? p.v_new : p.k_new;
   const bool whole = whole_tile(w, t0);
@@ -55,12 +62,63 @@ __device__ __forceinline__ void load_tile(const PagedParams& p, const Walk& w, i
     const HalfSource h = half_source(p, __builtin_amdgcn_readlane(pages, first + half), hp, kvh);
     const unsigned char* base = (h.paged ? cache : fresh) + h.offset;
     const bool plain = whole && !h.none;
+    const unsigned char* from[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const unsigned char* from = base + off[q];
-      if (!plain && (h.none || !walked(w, hp + 4 * q + (lane >> 4)))) from = g_zeros + ((lane & 15) << 4);
-      load_lds_from(from, dst + half * kHalfBytes + q * 1024);
+      from[q] = base + off[q];
+      if (!plain && (h.none || !walked(w, hp + 4 * q + (lane >> 4)))) from[q] = g_zeros + ((lane & 15) << 4);
     }
+    const uint32_t at = dst + half * kHalfBytes;
+    if (kept >> (first + half) & 1) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) load_lds_from(from[q], at + q * 1024);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) stream_lds_from(from[q], at + q * 1024);
+    }
+  }
+}
+
+// Sequences that share a prefix name the same first page.  For each of the first
+// kPartners sequences: another one with its first page, or -1.  (Found through a table of
+// the largest and the smallest such sequence of each page, by its low bits: one page's
+// sequences may hide another's, which then counts as not shared.)
+constexpr int kPartners = 512;
+constexpr int kPartnerPer = kPartners / kRowsThreads;
+
+struct Partners {
+  unsigned long long lo[kPartners], hi[kPartners];
+};
+
+__device__ __forceinline__ void first_pages(const PagedParams& p, int (&page)[kPartnerPer]) {
+#pragma unroll
+  for (int k = 0; k < kPartnerPer; ++k) {
+    const int s = threadIdx.x + k * kRowsThreads;
+    page[k] = s < p.n_segments && p.table_len > 0 ? p.tables[s * p.table_stride] : -1;
+  }
+}
+
+__device__ __forceinline__ void enter_partners(const int (&page)[kPartnerPer], Partners& t) {
+#pragma unroll
+  for (int k = 0; k < kPartnerPer; ++k) {
+    if (page[k] < 0) continue;
+    const unsigned long long key = (unsigned long long)page[k] << 32 | (threadIdx.x + k * kRowsThreads);
+    atomicMin(&t.lo[page[k] % kPartners], key);
+    atomicMax(&t.hi[page[k] % kPartners], key);
+  }
+}
+
+__device__ __forceinline__ void find_partners(const int (&page)[kPartnerPer], const Partners& t, int16_t* partner_of) {
+#pragma unroll
+  for (int k = 0; k < kPartnerPer; ++k) {
+    const int s = threadIdx.x + k * kRowsThreads;
+    int found = -1;
+    if (page[k] >= 0) {
+      const unsigned long long lo = t.lo[page[k] % kPartners], hi = t.hi[page[k] % kPartners];
+      if ((int)(lo >> 32) == page[k] && (int)lo != s) found = (int)lo;
+      if ((int)(hi >> 32) == page[k] && (int)hi != s) found = (int)hi;
+    }
+    partner_of[s] = (int16_t)found;
   }
 }
 
@@ -72,11 +130,27 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
   __shared__ int64_t wave_sum[kWaves];
+  __shared__ int16_t partner_of[kPartners];
+  static_assert(sizeof(Partners) <= sizeof(smem), "in the tiles' memory, before them");
   const Blocks blocks = p.narrow;
+  Partners& partners = *reinterpret_cast<Partners*>(smem);
+  int page0[kPartnerPer];
+  if (p.streamed) {
+    first_pages(p, page0);
+    for (int i = tid; i < kPartners; i += kRowsThreads) {
+      partners.lo[i] = ~0ull;
+      partners.hi[i] = 0;
+    }
+  }
   const Counted counted = count_steps<kRowsThreads, kWaves, kSetup>(p, blocks, wave_sum);
+  if (p.streamed) enter_partners(page0, partners);
   const Share share = find_share<kWaves, kSetup, 1, false>(p, blocks, counted, blockIdx.x);
   if (tid == 0) p.starts[blockIdx.x] = share.at;
   if (same(share.at, share.end)) return;
+  if (p.streamed) {
+    find_partners(page0, partners, partner_of);
+    __syncthreads();
+  }
 
   unsigned char* const mine = smem + wave * kWaveBytes;
   const uint32_t lds = lds_addr(mine);
@@ -104,18 +178,30 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   Walk w;
   int n_mine = 0;  // this wave's tiles: kWaves (step + j) + wave for j below n_mine
   int ids = -1;    // pages of the halves of tiles 32 (j / 32) .. of this wave, one per lane
+  int other = -1;  // and another sequence's there, if it shares the first page
+  int partner = -1;
+  uint64_t kept = ~0ull;  // halves that another sequence reads too
   int pos[NB];
   bf16x8 qf[NB][4];  // B of S^T = K Q^T: row i16 of block b, head dims 32 step + 8 g ..
   f32x4 o[8][NB];
   float m[NB], l[NB];
   auto tile_at = [&](int j) { return tile_begin(w, kWaves * (step + j) + wave); };
   auto fetch_ids = [&](int j) {
-    ids = -1;
+    ids = other = -1;
     const int jj = j + (lane >> 1);
-    if (jj < n_mine) ids = page_of(p, s, tile_at(jj) + (lane & 1) * kBlockTokens);
+    if (jj < n_mine) {
+      const int hp = tile_at(jj) + (lane & 1) * kBlockTokens;
+      ids = page_of(p, s, hp);
+      if (partner >= 0) other = page_of(p, Segment{0, 0, 0, 0, p.tables + partner * p.table_stride}, hp);
+    }
+  };
+  auto have_ids = [&]() {
+    landed(ids);
+    landed(other);
+    kept = p.streamed && w.n >= kStreamTiles ? __builtin_amdgcn_ballot_w64(ids == other) : ~0ull;
   };
   auto load = [&](int j, int tensor) {
-    load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), off, lane, lds + tensor * kTileBytes, tensor);
+    load_tile(p, w, tile_at(j), kvh, ids, 2 * (j & 31), kept, off, lane, lds + tensor * kTileBytes, tensor);
   };
   // The four waves' results, unnormalised, row by row through LDS: float4 c of row r at
   // slot c ^ (r % 16) of its row.
@@ -200,12 +286,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       }
       const int t_end = w.n < kWaves * stop ? w.n : kWaves * stop;
       n_mine = (t_end - kWaves * step - wave + kWaves - 1) / kWaves;
+      if (p.streamed) partner = __builtin_amdgcn_readfirstlane(x.seg < kPartners ? partner_of[x.seg] : -1);
       fetch_ids(0);
     }
     if (!first) store();
     if (!more) return;
     out = now;
-    landed(ids);
+    have_ids();
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -231,7 +318,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       if ((jn & ~31) != ids_of) {
         ids_of = jn & ~31;
         fetch_ids(ids_of);
-        landed(ids);
+        have_ids();
       }
       __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // K of tile j is in LDS
       asm volatile("" ::: "memory");

@@ -169,7 +169,7 @@ __device__ __forceinline__ int places(const Blocks& b) { return b.run * b.stride
 
 struct Block {
   Segment s;
-  int block;
+  int seg, block;
   bool rows;  // it has any
   int next;   // the first place after this one whose block may have rows
 };
@@ -178,6 +178,7 @@ __device__ __forceinline__ Block block_at(const PagedParams& p, const Blocks& b,
   Block x;
   const int i = b.run == 1 ? place : place % b.run * b.stride + place / b.run;
   const int seg = b.n == 1 ? i : (int)((unsigned)i / (unsigned)b.n);
+  x.seg = seg;
   x.block = i - seg * b.n;
   x.rows = false;
   x.next = place + 1;
@@ -333,6 +334,14 @@ __device__ __forceinline__ void load_lds_from(const void* addr, uint32_t lds_bas
   asm volatile(
       "s_nop 0\n\t"
       "global_load_lds_dwordx4 %0, off\n\t" ::"v"(addr),
+      "{m0}"(__builtin_amdgcn_readfirstlane((int)lds_base))
+      : "memory");
+}
+// The same with the non-temporal hint.
+__device__ __forceinline__ void stream_lds_from(const void* addr, uint32_t lds_base) {
+  asm volatile(
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, off nt\n\t" ::"v"(addr),
       "{m0}"(__builtin_amdgcn_readfirstlane((int)lds_base))
       : "memory");
 }

@@ -34,6 +34,7 @@ struct PagedParams {
   int32_t table_len;       // entries of a table
   const int32_t* tables;
   int64_t table_stride;
+  int32_t streamed;        // more pages than the Infinity Cache holds
   int32_t paged_end;       // positions below it are read through the table
   int32_t key_end;         // and from this one on there are no keys
 

@@ -315,6 +315,29 @@ def test_another_stream():
 
 # --- append ------------------------------------------------------------------------------
 
+@pytest.mark.parametrize("new", [1, 3])
+def test_shared_prefixes_in_a_large_pool(new):
+    """More pages than the Infinity Cache holds: long walks stream, but for the pages
+    that another sequence names too."""
+    b = Batch([1700, 1500, 1400, 2000, 60, 1300, 1700], [new] * 7, 8, 2, seed=89, uniform=True, spare=17000)
+    for s, tokens in ((1, 800), (2, 1392), (4, 48), (6, 16)):
+        b.tables[s, :tokens // B] = b.tables[0, :tokens // B]
+        b.k[s][:tokens], b.v[s][:tokens] = b.k[0][:tokens], b.v[0][:tokens]
+    b.tables[5, 3] = -1
+    b.k[5][48:64] = b.v[5][48:64] = 0
+    b.dev_tables.copy_(b.tables)
+    b.check(*b.run())
+    b.check(*b.run(1350, 20), 1350, 20)
+
+
+def test_many_sequences_in_a_large_pool():
+    rng = np.random.RandomState(9)
+    lens = rng.randint(1, 40, 602).tolist()
+    lens[3], lens[511], lens[512], lens[600] = 1400, 1500, 1600, 1333
+    b = Batch(lens, [1] * 602, 4, 2, seed=90, uniform=True, spare=17000)
+    b.check(*b.run())
+
+
 def test_two_calls_at_once():
     """Calls on two streams, each with its workspace, and a page copy beside them."""
     a = Batch([3000, 50, 900], [1, 1, 1], 8, 2, seed=86, uniform=True)
