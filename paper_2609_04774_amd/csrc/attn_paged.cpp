@@ -178,7 +178,7 @@ extern "C" int cp_attn_paged(const cp_paged_kv* kv, const void* q, int64_t q_str
     p.tables = kv->tables;
     p.table_stride = kv->table_stride;
     p.table_len = (int32_t)std::min<int64_t>(INT32_MAX, kv->table_stride);
-    p.streamed = 2 * kv->n_blocks > kInfinityCacheBytes / (kBlockTokens * p.kv_stride);
+    p.streamed = kv->n_blocks > kInfinityCacheBytes / (2 * kBlockTokens * p.kv_stride);
     p.paged_end = INT32_MAX;
     p.key_end = (int32_t)(std::min<int64_t>(kMaxTokens / kBlockTokens, kv->table_stride) * kBlockTokens);
     p.n_segments = kv->n_seqs;
