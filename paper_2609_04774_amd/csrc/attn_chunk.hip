@@ -3,8 +3,8 @@
 // those of attn_rows.hip; what differs is what bounds it, the matrix cores.
 //
 // A workgroup of 8 waves (two per SIMD: one's vector work issues while the other's
-// products run) owns a block of 256 or 384 rows of one KV head, 16 NB per wave, and walks
-// their keys in tiles of 32 that all waves read from LDS: every fragment of K or V that
+// products run) owns a block of 128, 256 or 384 rows of one KV head, 16 NB per wave, and
+// walks their keys in tiles of 32 that all waves read from LDS: every fragment of K or V that
 // is read feeds NB products, one for each 16 rows.  One iteration runs O += V_{j-1}^T P_{j-1}, the
 // softmax of tile j and S_{j+1} = K_{j+1} Q^T as one sequence of 16 slots, each
 // with one fragment, its products and a share of the vector work; the loads of tile
@@ -15,10 +15,12 @@
 //
 // Measured (32 query and 8 KV heads): 4096 rows after 32768 tokens (2.34 TFLOP) 1839 us,
 // 1270 TFLOP/s, where a product of two 8192 x 8192 matrices runs at 1210; 256 rows to a
-// block 1961.  A tile takes 0.93 us of 256 rows and 1.28 of 384, but those fit fewer
-// walks and pad more: alone, 4096 rows take 195 us with them and 173 without.  A
-// kernel that held both bodies had its registers spilled; so there are two, and the
-// first leaves the work to the second when the lengths say so.  A rank's 8192 rows
+// block 1961.  A tile takes 0.61 us of 128 rows, 0.93 of 256 and 1.28 of 384, and larger
+// blocks pad more and have fewer walks to share out: alone, 4096 rows take 195 us in
+// blocks of 384 and 173 in those of 256; 200 rows 24 of 256 and 20 of 128; 63 single tokens
+// after 256 to 32768 keys and a chunk of 2048 590 and 520.  So the lengths choose.  One
+// kernel holds the bodies of 128 and 256; with that of 384 its registers were spilled,
+// which is a second kernel that the first may leave the work to.  A rank's 8192 rows
 // through a window of 4096 440 us (0.41 TFLOP), 21 of them the merge.  One barrier for
 // two tiles against one each: 5 % faster.  KV heads one after another, blocks inside,
 // against the reverse: 4 to 7 %.
@@ -37,9 +39,10 @@ constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % 
 constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
 constexpr int kSetup = 10;  // of a walk, in tiles
 constexpr int kSnap = 4;   // tiles: a part costs its set-up, and its rows a merge
-// A wide block's tile takes 11/8 of a narrow one's (0.93 us).  A share of wide blocks
-// costs more besides, in tiles: its set-ups and its parts' merge are larger, and so
-// are, at both edges of a window, the tiles that some row sees in part.
+// A tile of 128, 256 and 384 rows takes 21/32, 1 and 11/8 of 0.93 us.  A share of larger
+// blocks costs more besides, in tiles: its set-ups and its parts' merge are larger, and
+// so are, at both edges of a window, the tiles that some row sees in part.
+constexpr int kNarrowSteps = 5;
 constexpr int kWideSteps = 40, kWideWindowSteps = 80;
 
 // LDS tiles by 16-byte columns: column c of a half holds chunk c of its 16 keys, key
@@ -195,35 +198,15 @@ __device__ __forceinline__ Walk uniform_walk(const Walk& w) {
   return Walk{u(w.end), u(w.lo), u(w.sink), u(w.p_lo), u(w.p_hi), u(w.n_sink_tiles), u(w.base), u(w.n)};
 }
 
-// Of a launch that may have wide blocks (p.wide) the kernel of narrow ones comes first,
-// and the lengths say which of the two does the work.
+// One workgroup's share, of blocks of 16 NB rows per wave.
 template <int NB>
-__global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParams p) {
+__device__ __forceinline__ void attend(const PagedParams& p, const Blocks& blocks, const Share& share, int number,
+                                       unsigned char* smem) {
   constexpr int kRows = 16 * NB * kWaves;
-  constexpr int kLookahead = NB == 2 ? 3 : 2;  // slots a fragment is read ahead of its products
-  constexpr bool kWide = kRows == kWideRows;
-  static_assert(kWide || kRows == kChunkRows, "the rows of a workgroup");
-  // The buffers of K, of V, and a V tile of zeros.
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[(2 * kBufs + 1) * kTileBytes];
-  __shared__ int64_t wave_sum[2][kWaves];
+  constexpr int kLookahead = NB == 1 ? 6 : NB == 2 ? 3 : 2;  // slots a fragment is read ahead of its products
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
-  const Blocks blocks = kWide ? p.wide : p.narrow;
-  if (kWide && *p.choice == 0) return;
-  // Shares are numbered so that an XCD's workgroups (every eighth) have neighbouring
-  // ones, whose walks meet in its L2.
-  const int number = p.n_shares % 8 == 0 ? (int)(blockIdx.x % 8) * (p.n_shares / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
-  const Counted counted = count_steps<kChunkThreads, 1, kSetup>(p, blocks, wave_sum[0]);
-  if (!kWide && p.choice) {
-    const Counted other = count_steps<kChunkThreads, 1, kSetup>(p, p.wide, wave_sum[1]);
-    const bool wide = other.total * 11 / 8 * p.Hkv + (p.window ? kWideWindowSteps : kWideSteps) * p.n_shares < counted.total * p.Hkv;
-    if (blockIdx.x == 0 && tid == 0) *p.choice = wide;
-    if (wide) return;
-  }
-  const Share share = find_share<1, kSetup, kSnap, true>(p, blocks, counted, number);
-  if (tid == 0) p.starts[number] = share.at;
-  if (same(share.at, share.end)) return;
 
   unsigned char* const kbuf = smem;
   unsigned char* const vbuf = smem + kBufs * kTileBytes;
@@ -509,13 +492,60 @@ __global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParam
   }
 }
 
+// The buffers of K, of V, and a V tile of zeros.
+struct Tiles {
+  unsigned char bytes[(2 * kBufs + 1) * kTileBytes];
+};
+
+// Shares are numbered so that an XCD's workgroups (every eighth) have neighbouring
+// ones, whose walks meet in its L2.
+__device__ __forceinline__ int share_number(const PagedParams& p) {
+  return p.n_shares % 8 == 0 ? (int)(blockIdx.x % 8) * (p.n_shares / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
+}
+
+// Looks at the lengths for the way to cut the rows, and does the work unless that is the
+// last of three.
+__global__ __launch_bounds__(kChunkThreads, 1) void attn_chunk_kernel(PagedParams p) {
+  __shared__ __attribute__((aligned(1024))) Tiles tiles;
+  const int number = share_number(p);
+  Counted counted[3];
+  count_steps<kChunkThreads, 1, kSetup>(p, p.n_ways, counted);
+  const int64_t narrow = counted[0].total * p.Hkv, middle = counted[1].total * p.Hkv, wide = counted[2].total * p.Hkv;
+  int way = narrow * 21 / 32 < middle + kNarrowSteps * p.n_shares ? 0 : 1;
+  if (p.n_ways == 3 && wide * 11 / 8 + (p.window ? kWideWindowSteps : kWideSteps) * p.n_shares < middle) way = 2;
+  way = __builtin_amdgcn_readfirstlane(way);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.choice = way;
+  if (way == 2) return;
+  const Blocks blocks = p.blocks[way];
+  const Share share = find_share<1, kSetup, kSnap, true>(p, blocks, way ? counted[1] : counted[0], number);
+  if (threadIdx.x == 0) p.starts[number] = share.at;
+  if (same(share.at, share.end)) return;
+  if (way == 0)
+    attend<1>(p, blocks, share, number, tiles.bytes);
+  else
+    attend<2>(p, blocks, share, number, tiles.bytes);
+}
+
+__global__ __launch_bounds__(kChunkThreads, 1) void attn_wide_kernel(PagedParams p) {
+  __shared__ __attribute__((aligned(1024))) Tiles tiles;
+  if (*p.choice != 2) return;
+  const int number = share_number(p);
+  Counted counted[3];
+  count_steps<kChunkThreads, 1, kSetup>(p, 3, counted);
+  const Blocks blocks = p.blocks[2];
+  const Share share = find_share<1, kSetup, kSnap, true>(p, blocks, counted[2], number);
+  if (threadIdx.x == 0) p.starts[number] = share.at;
+  if (same(share.at, share.end)) return;
+  attend<3>(p, blocks, share, number, tiles.bytes);
+}
+
 }  // namespace
 
 int launch_attn_chunk(const PagedParams& p, void* stream, const char* who) {
   const dim3 grid((unsigned)p.n_shares), block(kChunkThreads);
   hipStream_t st = (hipStream_t)stream;
-  hipLaunchKernelGGL(attn_chunk_kernel<kChunkRows / (16 * kWaves)>, grid, block, 0, st, p);
-  if (p.choice) hipLaunchKernelGGL(attn_chunk_kernel<kWideRows / (16 * kWaves)>, grid, block, 0, st, p);
+  hipLaunchKernelGGL(attn_chunk_kernel, grid, block, 0, st, p);
+  if (p.n_ways == 3) hipLaunchKernelGGL(attn_wide_kernel, grid, block, 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));
   return launch_attn_merge(p, stream, who);

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
   const ShareStart at = p.starts[share];
   ShareStart next = share + 1 + lane < p.n_shares ? p.starts[share + 1 + lane] : none;
   if (at.step == 0 || (same_walk(before, at) && before.step > 0)) return;
-  const Blocks& b = p.choice && *p.choice ? p.wide : p.narrow;
+  const Blocks& b = p.blocks[p.choice ? *p.choice : 0];
   const Block x = block_at(p, b, at.place);
   const Segment& s = x.s;
   const int r0 = kRows * (4 * blockIdx.y + (threadIdx.x >> 6));  // of the block
@@ -112,11 +112,11 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
 int launch_attn_merge(const PagedParams& p, void* stream, const char* who) {
   if (p.n_shares == 1) return CP_OK;
   const unsigned shares = (unsigned)p.n_shares - 1;
-  if (p.narrow.rows > 32)  // few parts of many rows
-    hipLaunchKernelGGL(share_merge_kernel<4>, dim3(shares, (unsigned)((p.choice ? p.wide.rows : p.narrow.rows) / 16)), dim3(256), 0,
+  if (p.choice)  // few parts of many rows
+    hipLaunchKernelGGL(share_merge_kernel<4>, dim3(shares, (unsigned)(p.blocks[p.n_ways - 1].rows / 16)), dim3(256), 0,
                        (hipStream_t)stream, p);
   else
-    hipLaunchKernelGGL(share_merge_kernel<1>, dim3(shares, (unsigned)(p.narrow.rows / 4)), dim3(256), 0,
+    hipLaunchKernelGGL(share_merge_kernel<1>, dim3(shares, (unsigned)(p.blocks[0].rows / 4)), dim3(256), 0,
                        (hipStream_t)stream, p);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CP_OK : fail(CP_ERR_HIP, std::string(who) + " launch: " + hipGetErrorString(e));

@@ -47,25 +47,25 @@ int set_common(PagedParams* p, const std::string& who, int32_t Hq, int32_t Hkv, 
 // 32 with the kernel of few rows; else those of the other.
 int block_rows(int64_t max_q, int32_t G) {
   const int64_t rows = max_q * G;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : kChunkRows;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : kChunkRows[0];
 }
-int shares_of(int block_rows) { return block_rows == kChunkRows ? kChunkShares : kRowsShares; }
+int shares_of(int block_rows) { return block_rows == kChunkRows[0] ? kChunkShares : kRowsShares; }
 
-// Whether wide blocks (the lengths decide on them) are worth a second kernel's launch, 4 us
+// Ways to cut the rows into blocks, of which the lengths choose.  The widest blocks are
+// worth a second kernel's launch to long calls, 4 us
 // where it has nothing to do.  One prompt's 4096 rows of 32 and 8 heads with and without
 // the choice: alone 203 and 204 us, after 8K tokens 654 and 684, after 32K 1839 and 1961;
 // 2048 rows alone 84 and 80, after 8K 315 and 316, after 32K 978 and 1016.
-bool may_be_wide(int block_rows, int64_t n_rows, int32_t Hq) {
-  return block_rows == kChunkRows && n_rows * Hq >= 131072;
+int ways_of(int block_rows, int64_t n_rows, int32_t Hq) {
+  return block_rows != kChunkRows[0] ? 1 : n_rows * Hq >= 131072 ? 3 : 2;
 }
 
 // The shares' starts and, behind them, the choice of blocks.
 size_t starts_bytes(int shares) { return ((size_t)shares * sizeof(ShareStart) + 255) / 256 * 256 + 256; }
 
 size_t workspace_bytes_of(int64_t n_rows, int64_t max_q, int32_t Hq, int32_t G) {
-  const int rows = block_rows(max_q, G);
-  return starts_bytes(shares_of(rows)) +
-         2 * (size_t)shares_of(rows) * slot_floats(may_be_wide(rows, n_rows, Hq) ? kWideRows : rows) * 4;
+  const int rows = block_rows(max_q, G), ways = ways_of(rows, n_rows, Hq);
+  return starts_bytes(shares_of(rows)) + 2 * (size_t)shares_of(rows) * slot_floats(ways > 1 ? kChunkRows[ways - 1] : rows) * 4;
 }
 
 // How a launch is cut into blocks of so many rows.
@@ -80,7 +80,7 @@ Blocks cut(const PagedParams& p, int rows) {
   // 1977 us, 2132; through a window of 4096 433, 459.
   const int64_t full = p.n_rows * p.G / rows;
   const int64_t run = places * p.Hkv / p.n_shares;
-  b.run = rows >= kChunkRows && run > 1 && 2 * full >= places ? (int32_t)run : 1;
+  b.run = rows >= kChunkRows[0] && run > 1 && 2 * full >= places ? (int32_t)run : 1;
   b.stride = (int32_t)((places + b.run - 1) / b.run);
   return b;
 }
@@ -96,16 +96,14 @@ int launch(PagedParams* p, const std::string& who, int64_t max_q, void* workspac
     return fail(CP_ERR_UNSUPPORTED, who + "too many sequences of so many rows");
   p->max_q = (int32_t)max_q;
   p->n_shares = shares_of(rows);
-  p->narrow = cut(*p, rows);
   unsigned char* const slots = static_cast<unsigned char*>(workspace) + starts_bytes(p->n_shares);
-  if (may_be_wide(rows, p->n_rows, p->Hq)) {
-    p->wide = cut(*p, kWideRows);
-    p->choice = reinterpret_cast<int32_t*>(slots - 256);
-  }
+  p->n_ways = ways_of(rows, p->n_rows, p->Hq);
+  for (int y = 0; y < p->n_ways; ++y) p->blocks[y] = cut(*p, p->n_ways > 1 ? kChunkRows[y] : rows);
+  if (p->n_ways > 1) p->choice = reinterpret_cast<int32_t*>(slots - 256);
   p->starts = static_cast<ShareStart*>(workspace);
   p->slots = reinterpret_cast<float*>(slots);
   const std::string name = who.substr(0, who.size() - 2);
-  return rows == kChunkRows ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
+  return p->n_ways > 1 ? launch_attn_chunk(*p, stream, name.c_str()) : launch_attn_rows(*p, stream, name.c_str());
 }
 
 // The most rows of a sequence, from a batch's arguments.

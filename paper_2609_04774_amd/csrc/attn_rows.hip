@@ -129,10 +129,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
-  __shared__ int64_t wave_sum[kWaves];
   __shared__ int16_t partner_of[kPartners];
   static_assert(sizeof(Partners) <= sizeof(smem), "in the tiles' memory, before them");
-  const Blocks blocks = p.narrow;
+  const Blocks blocks = p.blocks[0];
   Partners& partners = *reinterpret_cast<Partners*>(smem);
   int page0[kPartnerPer];
   if (p.streamed) {
@@ -142,9 +141,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       partners.hi[i] = 0;
     }
   }
-  const Counted counted = count_steps<kRowsThreads, kWaves, kSetup>(p, blocks, wave_sum);
+  Counted counted[1];
+  count_steps<kRowsThreads, kWaves, kSetup>(p, 1, counted);
   if (p.streamed) enter_partners(page0, partners);
-  const Share share = find_share<kWaves, kSetup, 1, false>(p, blocks, counted, blockIdx.x);
+  const Share share = find_share<kWaves, kSetup, 1, false>(p, blocks, counted[0], blockIdx.x);
   if (tid == 0) p.starts[blockIdx.x] = share.at;
   if (same(share.at, share.end)) return;
   if (p.streamed) {
@@ -402,7 +402,7 @@ int launched(const char* who) {
 int launch_attn_rows(const PagedParams& p, void* stream, const char* who) {
   const dim3 grid((unsigned)p.n_shares), block(kRowsThreads);
   hipStream_t st = (hipStream_t)stream;
-  if (p.narrow.rows == 16)
+  if (p.blocks[0].rows == 16)
     hipLaunchKernelGGL(attn_rows_kernel<1>, grid, block, 0, st, p);
   else
     hipLaunchKernelGGL(attn_rows_kernel<2>, grid, block, 0, st, p);

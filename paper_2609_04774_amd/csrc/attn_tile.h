@@ -235,36 +235,45 @@ __device__ __forceinline__ int cost_of(const PagedParams& p, const Blocks& b, co
   return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, b, x.s, x.block)) : 0;
 }
 
-template <int kThreads, int kTiles, int kSetup>
-__device__ Counted count_steps(const PagedParams& p, const Blocks& b, int64_t (&wave_sum)[kThreads / 64]) {
+// In each of the launch's first kWays ways to cut the rows.
+template <int kThreads, int kTiles, int kSetup, int kWays>
+__device__ void count_steps(const PagedParams& p, int ways, Counted (&counted)[kWays]) {
+  __shared__ int64_t wave_sum[kWays][kThreads / 64];
   const int tid = threadIdx.x;
-  const int n_places = places(b);
-  Counted c;
-  c.per = (n_places + kThreads - 1) / kThreads;
-  c.i0 = tid * c.per < n_places ? tid * c.per : n_places;
-  c.i1 = c.i0 + c.per < n_places ? c.i0 + c.per : n_places;
-  c.mine = 0;
-  for (int i = c.i0; i < c.i1;) {
-    const Block x = block_at(p, b, i);
-    c.mine += cost_of<kTiles, kSetup>(p, b, x);
-    i = x.next;
-  }
-  c.before = c.mine;
 #pragma unroll
-  for (int k = 1; k < 64; k *= 2) {
-    const int64_t x = __shfl_up(c.before, k);
-    if ((tid & 63) >= k) c.before += x;
+  for (int y = 0; y < kWays; ++y) {
+    const Blocks& b = p.blocks[y];
+    const int n_places = y < ways ? places(b) : 0;
+    Counted& c = counted[y];
+    c.per = (n_places + kThreads - 1) / kThreads;
+    c.i0 = tid * c.per < n_places ? tid * c.per : n_places;
+    c.i1 = c.i0 + c.per < n_places ? c.i0 + c.per : n_places;
+    c.mine = 0;
+    for (int i = c.i0; i < c.i1;) {
+      const Block x = block_at(p, b, i);
+      c.mine += cost_of<kTiles, kSetup>(p, b, x);
+      i = x.next;
+    }
+    c.before = c.mine;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+      const int64_t x = __shfl_up(c.before, k);
+      if ((tid & 63) >= k) c.before += x;
+    }
+    if ((tid & 63) == 63) wave_sum[y][tid >> 6] = c.before;
   }
-  if ((tid & 63) == 63) wave_sum[tid >> 6] = c.before;
   __syncthreads();
-  c.total = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < (tid >> 6)) c.before += wave_sum[w];
-    c.total += wave_sum[w];
+  for (int y = 0; y < kWays; ++y) {
+    Counted& c = counted[y];
+    c.total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+      if (w < (tid >> 6)) c.before += wave_sum[y][w];
+      c.total += wave_sum[y][w];
+    }
+    c.before -= c.mine;
   }
-  c.before -= c.mine;
-  return c;
 }
 
 // The thread whose places hold a share's end finds the walk there.

@@ -56,9 +56,9 @@ struct PagedParams {
   // Workspace: where each workgroup's share of the walks begins, then two slots of
   // partial results per workgroup.
   int32_t n_shares;
-  Blocks narrow;           // how the rows are cut into blocks,
-  Blocks wide;             // or in wide ones
-  int32_t* choice;         // of the two (1: wide), by the lengths; null: narrow
+  Blocks blocks[3];        // ways to cut the rows into blocks: of 16 or 32 rows, or
+  int32_t n_ways;          // (kChunkRows) two or three
+  int32_t* choice;         // of these, by the lengths; null: the first
   struct ShareStart* starts;
   float* slots;
 };
@@ -71,8 +71,8 @@ struct ShareStart {
 
 constexpr int kRowsThreads = 256;
 constexpr int kChunkThreads = 512;
-constexpr int kChunkRows = 256;    // rows of a block of the kernel of many rows,
-constexpr int kWideRows = 384;     // or of a long launch's
+// Rows of a block of the kernels of many rows; the last only for long launches.
+constexpr int kChunkRows[3] = {128, 256, 384};
 constexpr int kRowsShares = 512;   // workgroups: two per compute unit
 constexpr int kChunkShares = 256;  // one
 

@@ -153,13 +153,46 @@ def test_a_long_chunk_among_many_sequences():
     b.check(*b.run(50, 4), 50, 4, rows=np.array([0, 1, 31, 32, 300, 699]))
 
 
-def wide(b, window=0, n_sink=0):
-    """A launch whose lengths choose wide blocks (the workspace says so behind the
-    256 shares' starts)."""
+def blocks_of(rows, b, window=0, n_sink=0):
+    """A launch whose lengths choose blocks of so many rows (the workspace says which,
+    behind the 256 shares' starts)."""
     ws = torch.empty(cp.attn_paged_workspace_size(b.kv, len(b.q), b.max_q, b.Hq), dtype=torch.uint8, device=DEV)
     out = b.run(window, n_sink, ws=ws)
-    assert ws.view(torch.int32)[1024] == 1
+    assert ws.view(torch.int32)[1024] == [128, 256, 384].index(rows)
     return out
+
+
+def wide(b, window=0, n_sink=0):
+    return blocks_of(384, b, window, n_sink)
+
+
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (1000, 0), (1100, 40)])
+def test_blocks_of_256_rows(window, n_sink):
+    b = Batch([1500, 1400, 1600, 1211, 50, 1550, 850, 1400], [250, 256, 255, 300, 0, 512, 1, 256], 64, 64, seed=91)
+    rows = np.array([0, 1, 31, 32, 100, 127, 128, 200, 249, 255, 256, 299, 511])
+    if window:
+        b.hide(window, n_sink)
+    b.check(*blocks_of(256, b, window, n_sink), window, n_sink, rows=rows)
+
+
+@pytest.mark.parametrize("rows,heads,new", [(128, 2, 100), (256, 64, 256)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_values_in_blocks(rows, heads, new, bad):
+    """As above, in blocks of many rows: an infinite or NaN value of one head."""
+    n = 5
+    b = Batch([777] * n, [new] * n, heads, heads, seed=92, uniform=True)
+    for s in range(n):
+        b.v[s][777 - new // 2, 1, 9] = bad
+    starts = torch.arange(0, 777 * n + 1, 777, dtype=torch.int32, device=DEV)
+    cp.kv_append(b.kv, torch.cat(b.k).to(DEV), torch.cat(b.v).to(DEV), q_start=starts)
+    o, lse = blocks_of(rows, b)
+    got = o.float().view(n, new, heads, D)
+    seen = got[:, new - new // 2:, 1, 9]
+    assert torch.isnan(seen).all() if np.isnan(bad) else (seen == bad).all()
+    finite = torch.isfinite(got)
+    finite[:, new - new // 2:, 1, 9] = True
+    assert finite.all()
+    b.check(o, lse, rows=np.array([0, 1, new // 2 - 1, new // 2, new - new // 2 - 1, new - new // 2, new - 1]))
 
 
 def test_wide_blocks():
@@ -209,13 +242,13 @@ def test_captured_launch_follows_the_choice_of_blocks():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         step()
-    for length, choice in ((17300, 1), (8192, 0), (5000, 0), (17300, 1)):
+    for length, is_wide in ((17300, True), (8192, False), (5000, False), (17300, True)):
         b.kv_len[0] = length
         b.dev_len.fill_(length)
         o.fill_(float("nan"))
         graph.replay()
         torch.cuda.synchronize()
-        assert int(ws.view(torch.int32)[1024]) == choice
+        assert (ws.view(torch.int32)[1024] == 2) == is_wide
         got = o.clone(), lse.clone()
         k, v = b.k[0], b.v[0]
         b.k[0], b.v[0] = k[:length], v[:length]
