@@ -51,9 +51,9 @@ int block_rows(int64_t max_q, int32_t G) {
 }
 int shares_of(int block_rows) { return block_rows == kChunkRows[0] ? kChunkShares : kRowsShares; }
 
-// Ways to cut the rows into blocks, of which the lengths choose.  The widest blocks are
-// worth a second kernel's launch to long calls, 4 us
-// where it has nothing to do.  One prompt's 4096 rows of 32 and 8 heads with and without
+// Ways to cut the rows into blocks, of which the lengths choose.  The widest blocks
+// are worth a second kernel's launch (4 us where it has nothing to do) to calls of many
+// rows only.  One prompt's 4096 rows of 32 and 8 heads with and without
 // the choice: alone 203 and 204 us, after 8K tokens 654 and 684, after 32K 1839 and 1961;
 // 2048 rows alone 84 and 80, after 8K 315 and 316, after 32K 978 and 1016.
 int ways_of(int block_rows, int64_t n_rows, int32_t Hq) {

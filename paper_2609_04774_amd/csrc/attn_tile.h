@@ -235,7 +235,7 @@ __device__ __forceinline__ int cost_of(const PagedParams& p, const Blocks& b, co
   return x.rows ? kSetup + steps_of<kTiles>(block_walk(p, b, x.s, x.block)) : 0;
 }
 
-// In each of the launch's first kWays ways to cut the rows.
+// For each of the launch's ways to cut the rows, at most kWays.
 template <int kThreads, int kTiles, int kSetup, int kWays>
 __device__ void count_steps(const PagedParams& p, int ways, Counted (&counted)[kWays]) {
   __shared__ int64_t wave_sum[kWays][kThreads / 64];
