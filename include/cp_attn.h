@@ -482,6 +482,9 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  *   workspace   device, 256-byte aligned, of the size above; it holds partial
  *               results while the call's kernels run: calls that may overlap
  *               (other streams, graphs replayed side by side) need their own.
+ * Scores, weights and sums are fp32.  The weights are rounded to bf16 for their
+ * product with the values, and O is divided by the sum of the rounded ones (as in
+ * cp_attn_partial): a mean of the values, rounded to bf16.
  * A row that sees no key has O = 0, LSE = -inf; a NaN among its scores gives O =
  * NaN, LSE = -inf.  Keys and values that a row does not see have no effect on
  * it, whatever they hold.  Scores (scaled) may be up to 10^9 in size: far beyond

@@ -12,6 +12,9 @@
 // the tiles before, which needs no look at the tile's own scores: they stay exact
 // relative to each other at any size, so only a tile whose weights could
 // overflow is done again with its own maximum (as in attn_partial.hip).
+// The sum of the rounded weights, which divides O, is one more product per 16 rows and
+// tile (2 to 3 % of a long launch; added up by vector instructions 6 to 14 %, by
+// 4 x 4 x 4 products 3 to 5 %).
 //
 // Measured (32 query and 8 KV heads): 4096 rows after 32768 tokens (2.34 TFLOP) 1839 us,
 // 1270 TFLOP/s, where a product of two 8192 x 8192 matrices runs at 1210; 256 rows to a
@@ -130,7 +133,8 @@ __device__ __forceinline__ void qk_tile(const unsigned char* buf, const Fragment
 // Raises the running maxima to a tile's own where that is higher; O and the sums
 // follow.
 template <int NB>
-__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], f32x4 (&o)[8][NB], float sl2) {
+__device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], float (&l)[NB], float (&mass)[NB],
+                                          f32x4 (&o)[8][NB], float sl2) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     float top = s[b][0][0];
@@ -139,6 +143,7 @@ __device__ __forceinline__ void raise_max(const Scores<NB>& s, float (&m)[NB], f
     const float m_new = __builtin_elementwise_maximum(m[b], quad_max(top) * sl2);
     const float alpha = __builtin_amdgcn_exp2f(m[b] - m_new);
     l[b] *= alpha;
+    mass[b] *= alpha;
 #pragma unroll
     for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
     m[b] = m_new;
@@ -159,7 +164,9 @@ __device__ __forceinline__ void finish(const Weights<NB>& w, float (&l)[NB], bf1
 
 template <int NB>
 __device__ __forceinline__ void pv_tile(const unsigned char* buf, const Fragments& f, const bf16x8 (&pf)[NB],
-                                        f32x4 (&o)[8][NB]) {
+                                        float (&mass)[NB], f32x4 (&o)[8][NB]) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) mass[b] += weight_sum(pf[b]);
 #pragma unroll
   for (int db = 0; db < 8; ++db) {
     const bf16x8 v = load_v(buf, f, db);
@@ -248,6 +255,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
   bf16x8 qf[NB][4];
   f32x4 o[8][NB];
   float m[NB], l[NB];
+  float mass[NB];  // sums of the rounded weights, of all four lanes of a row
   bf16x8 pf[NB];
 
   auto fetch_ids = [&](int j) {
@@ -299,7 +307,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
       const int r = out.r0 + 16 * b + i16;
       const float sum = quad_sum(l[b]);
       const bool live = m[b] > 0.5f * kNoMax && sum > 0.f;
-      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
+      const float inv = live ? 1.f / mass[b] : (sum != sum ? sum : 0.f);
       const float lse = live ? m[b] * kLn2 + logf(sum) : -INFINITY;
       if (out.slot) {
         const int rb = 16 * (NB * wave + b) + i16;
@@ -369,7 +377,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
       for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
       pf[b] = bf16x8{};
       m[b] = kNoMax;
-      l[b] = 0.f;
+      l[b] = mass[b] = 0.f;
     }
 
     if (n > 0) {
@@ -386,7 +394,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
         if (active) {
           qk_tile(k_now, fr, qf, sa);
           mask(j, sa);
-          raise_max(sa, m, l, o, sl2);
+          raise_max(sa, m, l, mass, o, sl2);
         }
         if (__builtin_expect(apart(j), 0)) {
           load(j + kAhead);
@@ -394,6 +402,8 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
 #pragma unroll
             for (int u = 0; u < 12 * NB; ++u) softmax_unit(u, sa, wt, m, sl2);
             finish(wt, l, pf);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mass[b] += weight_sum(pf[b]);
             pv_not_finite<NB>([&](int db) { return load_v(v_now, fr, db); }, pf, o);
           }
           ++j;
@@ -411,6 +421,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
           const unsigned char* v_this = vbuf + (j & (kBufs - 1)) * kTileBytes;
           load(j + kAhead);
           bf16x8 f[16];
+          f32x4 sums;  // of a block's rounded weights; added two slots later
 #pragma unroll
           for (int x = 0; x < kLookahead; ++x) f[x] = pre[x];
 #pragma unroll
@@ -425,6 +436,10 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
             if (slot < 8) {
 #pragma unroll
               for (int b = 0; b < NB; ++b) o[slot][b] = mfma16(f[slot], pf[b], o[slot][b]);
+              if (slot % 2 == 0) {
+                if (slot > 0 && slot / 2 <= NB) mass[slot / 2 - 1] += sums[0];
+                if (slot / 2 < NB) sums = weight_sums(pf[slot / 2]);
+              }
             } else {
               qk_step(s_out, f[slot], qf, slot - 8);
             }
@@ -439,7 +454,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
           if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
             qk_tile(kbuf + (j & (kBufs - 1)) * kTileBytes, fr, qf, s_in);
             mask(j, s_in);
-            raise_max(s_in, m, l, o, sl2);
+            raise_max(s_in, m, l, mass, o, sl2);
 #pragma unroll
             for (int u = 0; u < 12 * NB; ++u) softmax_unit(u, s_in, wt, m, sl2);
           }
@@ -464,7 +479,7 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
             if (++j >= n || apart(j)) break;
             mask(j, sa);
           }
-          pv_tile(v_before, fr, pf, o);
+          pv_tile(v_before, fr, pf, mass, o);
         } else {
           for (;;) {
             __builtin_amdgcn_s_waitcnt(wait_vm(2 * (kAhead - 3)));

@@ -6,8 +6,9 @@
 // or among the first tokens):  x_j = scale q.k_j,  LSE = ln sum_j e^{x_j},
 // O = sum_j e^{x_j - LSE} v_j, in one pass with a running maximum and sum (Milakov
 // & Gimelshein 2018; Dao 2023).  Scores, statistics and O are fp32; the weights
-// are rounded to bf16 for the second product (half a step at most, 2^-8 of each), O is
-// rounded once more as it is stored.
+// are rounded to bf16 for the second product (half a step at most, 2^-8 of each), and O
+// is divided by the sum of the rounded ones, so that it is a mean of the values whatever
+// the roundings; LSE takes the sum before them.  O is rounded once more as it is stored.
 //
 // Bound by HBM: 512 bytes per key and KV head, each read once, for 16 or 32 rows.
 // The walks of all blocks, in steps of 128 keys, are cut into equal parts,
@@ -125,7 +126,7 @@ __device__ __forceinline__ void find_partners(const int (&page)[kPartnerPer], co
 template <int NB>
 __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams p) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * kWaveBytes];
-  __shared__ float stat[2][kWaves][16 * NB];  // per wave and row: maximum, sum
+  __shared__ float stat[3][kWaves][16 * NB];  // per wave and row: maximum, sum, sum of the rounded weights
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, i16 = lane & 15;
@@ -185,6 +186,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
   bf16x8 qf[NB][4];  // B of S^T = K Q^T: row i16 of block b, head dims 32 step + 8 g ..
   f32x4 o[8][NB];
   float m[NB], l[NB];
+  float mass[NB];  // sums of the rounded weights, of all four lanes of a row
   auto tile_at = [&](int j) { return tile_begin(w, kWaves * (step + j) + wave); };
   auto fetch_ids = [&](int j) {
     ids = other = -1;
@@ -213,6 +215,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       if (g == 0) {
         stat[0][wave][r] = m[b];
         stat[1][wave][r] = sum;
+        stat[2][wave][r] = mass[b];
       }
 #pragma unroll
       for (int db = 0; db < 8; ++db)
@@ -224,18 +227,19 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       float top = kNoMax;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) top = __builtin_elementwise_maximum(top, stat[0][k][r]);
-      float sum = 0.f;
+      float sum = 0.f, rounded = 0.f;
       f32x4 a0 = {}, a1 = {};
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
         const float wk = __builtin_amdgcn_exp2f(stat[0][k][r] - top);
         sum += wk * stat[1][k][r];
+        rounded += wk * stat[2][k][r];
         const unsigned char* row = smem + k * kWaveBytes + r * (kHeadDim * 4);
         a0 += wk * *reinterpret_cast<const f32x4*>(row + ((c ^ (r & 15)) << 4));
         a1 += wk * *reinterpret_cast<const f32x4*>(row + (((c + 1) ^ (r & 15)) << 4));
       }
       const bool live = top > 0.5f * kNoMax && sum > 0.f;  // false for a NaN too
-      const float inv = live ? 1.f / sum : (sum != sum ? sum : 0.f);
+      const float inv = live ? 1.f / rounded : (sum != sum ? sum : 0.f);
       const float lse = live ? top * kLn2 + logf(sum) : -INFINITY;
       a0 *= inv;
       a1 *= inv;
@@ -307,7 +311,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
 #pragma unroll
       for (int db = 0; db < 8; ++db) o[db][b] = f32x4{};
       m[b] = kNoMax;
-      l[b] = 0.f;
+      l[b] = mass[b] = 0.f;
     }
     const unsigned char* kt = mine;
     const unsigned char* vt = mine + kTileBytes;
@@ -362,6 +366,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
           pf[b][r] = (__bf16)x;
         }
         l[b] = l[b] * alpha + sum;
+        mass[b] = mass[b] * alpha + weight_sum(pf[b]);
 #pragma unroll
         for (int db = 0; db < 8; ++db) o[db][b] *= alpha;
       }

@@ -395,6 +395,16 @@ __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// Sums of a tile's rounded weights P^T, each row's in its four lanes: the product of
+// ones with them.
+__device__ __forceinline__ f32x4 weight_sums(const bf16x8& pf) {
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
+  return mfma16(ones, pf, f32x4{});
+}
+__device__ __forceinline__ float weight_sum(const bf16x8& pf) { return weight_sums(pf)[0]; }
+
 // A of S^T = K Q^T: key i of the half, head dims 32 step + 8 g ..
 __device__ __forceinline__ bf16x8 k_frag(const unsigned char* k, int lane, int half, int step) {
   const int g = lane >> 4, i = lane & 15;
