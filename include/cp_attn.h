@@ -589,7 +589,8 @@ int cp_kv_copy_pages(void* const* caches, int32_t n_caches, int64_t n_blocks, in
  * before (Sec. 8: blocks are reserved before KV states are installed).  The
  * sequences are served in the order of the list until one asks for more pages
  * than are left: it and those after it that need pages get nothing, as does one
- * whose table is too short or whose add is negative, and keep their length.
+ * whose table is too short, whose add is negative, or whose last page, filled in
+ * part, was given back (more tokens would begin in it), and keep their length.
  * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
  */
 int cp_kv_reserve(const cp_kv_pool* pool, const int32_t* seqs, const int32_t* add, int64_t n, int32_t* missing,
@@ -614,7 +615,8 @@ int cp_kv_fork(const cp_kv_pool* pool, void* const* caches, int32_t n_caches, in
  * end[i]): their entries become -1, and a page that no other table names is free
  * (Sec. 8: blocks are released; behind a sliding window: begin = n_sink, end =
  * kv_len - window).  The page that holds the last token is given back if end
- * reaches kv_len; with begin <= 0 too the sequence is empty and its kv_len 0.
+ * reaches kv_len; with begin <= 0 too the sequence is empty and its kv_len 0.  Else
+ * kv_len stays, and unless it ends on a page the sequence takes no more tokens.
  * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
  */
 int cp_kv_free(const cp_kv_pool* pool, const int32_t* seqs, const int32_t* begin, const int32_t* end, int64_t n,

@@ -22,10 +22,14 @@ class Pool:
         self.caches = [c.copy() for c in caches]
         self.width = len(self.tables[0]) if self.tables else 0
 
-    def _take(self, n, end):
-        """The lowest n free pages, or None; `end`: pages asked for so far."""
+    def _take(self, n):
+        """The lowest n free pages, or None."""
         free = [p for p, r in enumerate(self.refs) if r == 0]
         return free[:n] if n <= len(free) else None
+
+    def _partial_page_gone(self, table, length):
+        """The last page is filled in part and the table does not name it."""
+        return length % B > 0 and not 0 <= table[length // B] < len(self.refs)
 
     def reserve(self, seqs, add):
         missing, seen, out = 0, set(), False
@@ -35,11 +39,11 @@ class Pool:
             seen.add(s)
             to = self.kv_len[s] + a
             first, last = -(-self.kv_len[s] // B), -(-to // B)
-            if a < 0 or last > self.width:
+            if a < 0 or last > self.width or (a > 0 and self._partial_page_gone(self.tables[s], self.kv_len[s])):
                 missing += 1
                 continue
             n = last - first
-            pages = None if out and n else self._take(n, None)
+            pages = None if out and n else self._take(n)
             if pages is None:
                 out, missing = True, missing + 1
                 continue
@@ -64,7 +68,7 @@ class Pool:
             whole, part = divmod(length, B)
             if part and whole < self.width and not 0 <= before[0][a][whole] < len(self.refs):
                 part = 0  # the parent's last page is not there: nothing to copy
-            pages = None if out and part else self._take(1 if part else 0, None)
+            pages = None if out and part else self._take(1 if part else 0)
             if -(-length // B) > self.width:
                 pages, bad = None, True
             else:

@@ -271,3 +271,52 @@ def test_serving_loop():
     step({2: 200, 3: 4, 0: 1}, W)
     count = torch.zeros_like(b.refs).index_add_(0, b.tables[b.tables >= 0].long(), torch.ones_like(b.tables[b.tables >= 0]))
     assert torch.equal(count, b.refs)
+
+
+def test_reserve_where_the_last_page_is_gone():
+    """A sequence whose last page, filled in part, was given back: more tokens have no
+    place in it.  The entry is missing and changes nothing; one that adds nothing, one
+    whose length ends on a page and the other entries of the list are served."""
+    b = Both(5, 8, 40, seed=10)
+    b.reserve([0, 1, 2, 3], [37, 32, 45, 20])
+    b.free([0, 1, 2], [5, 16, 32], [37, 32, 45])      # their last pages, the lengths stay
+    b.reserve([0, 1, 2, 3], [1, 1, 40, 1])
+    assert b.missing.tolist() == [2] and b.kv_len.tolist() == [37, 33, 45, 21, 0]
+    b.reserve([0, 2], [0, 0])
+    assert b.missing.tolist() == [0]
+    b.tables[3, 1], b.want.tables[3][1] = 40, 40      # no page of the pool either
+    cp.kv_reserve(b.pool, i32([3]), i32([1]), b.missing)
+    assert b.missing.tolist() == [1] and b.want.reserve([3], [1]) == 1 and b.kv_len.tolist() == b.want.kv_len
+
+
+def test_tokens_reserved_are_tokens_kept():
+    """Free, reserve, append, attend: what reserve says it has served is in the cache."""
+    Hq, Hkv = 8, 2
+    b = Both(3, 8, 40, n_caches=2, Hkv=Hkv, seed=11)
+    kv = cp.PagedKV(b.caches[0], b.caches[1], b.tables, b.kv_len)
+    g = torch.Generator().manual_seed(12)
+    b.reserve([0, 1, 2], [37, 48, 40])
+    b.free([0, 1], [5, 32], [37, 48])
+    before = b.kv_len.tolist()
+    cp.kv_reserve(b.pool, i32([0, 1, 2]), i32([9, 9, 9]), b.missing)
+    grown = [n > m for n, m in zip(b.kv_len.tolist(), before)]
+    assert b.missing.tolist() == [grown.count(False)]
+    k, v = randn(g, 27, Hkv, D), randn(g, 27, Hkv, D)
+    cp.kv_append(kv, k.to(DEV), v.to(DEV))
+    for s in range(3):
+        if grown[s]:
+            for i in range(9):
+                p = b.kv_len.tolist()[s] - 9 + i
+                page = int(b.tables[s, p // B])
+                assert page >= 0 and torch.equal(b.caches[0][page, p % B].cpu(), k[9 * s + i])
+                assert torch.equal(b.caches[1][page, p % B].cpu(), v[9 * s + i])
+    # A window of the appended tokens: attention reads what was appended.
+    o, lse = torch.empty(27, Hq, D, dtype=torch.bfloat16, device=DEV), torch.empty(27, Hq, device=DEV)
+    q = randn(g, 27, Hq, D)
+    ws = torch.empty(cp.attn_paged_workspace_size(kv, 27, 9, Hq), dtype=torch.uint8, device=DEV)
+    cp.attn_paged(kv, q.to(DEV), o, ws, lse=lse, window=9)
+    for s in range(3):
+        if grown[s]:
+            r = slice(9 * s + 8, 9 * s + 9)
+            want = owin.attend(f64(q)[r], [8], f64(k)[9 * s:9 * s + 9], f64(v)[9 * s:9 * s + 9], np.arange(9))
+            compare(f64(o)[r], f64(lse)[r], want, 9, f"sequence {s}")
