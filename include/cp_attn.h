@@ -601,9 +601,9 @@ int cp_kv_reserve(const cp_kv_pool* pool, const int32_t* seqs, const int32_t* ad
  * share the blocks of a common prefix): it shares the pages that the parent
  * has filled, receives a copy (in every cache) of a last page that is filled in
  * part, and has the parent's length.  Its own table row is overwritten: a child
- * must hold no pages (cp_kv_free).  A child that is also a parent in the list, or
- * whose copy finds no free page, gets nothing: an empty row, length 0 (a
- * parent of the list: unchanged).
+ * must hold no pages (cp_kv_free).  A child that is also a parent in the list, whose
+ * copy finds no free page, or whose parent's last page, filled in part, was given
+ * back, gets nothing: an empty row, length 0 (a parent of the list: unchanged).
  *   caches, n_caches, page_bytes  as in cp_kv_copy_pages; n_caches may be 0.
  * Errors: CP_ERR_INVALID, CP_ERR_UNSUPPORTED (n > CP_KV_MAX_LIST), CP_ERR_HIP.
  */

@@ -66,13 +66,10 @@ class Pool:
                 continue
             length = before[1][a]
             whole, part = divmod(length, B)
-            if part and whole < self.width and not 0 <= before[0][a][whole] < len(self.refs):
-                part = 0  # the parent's last page is not there: nothing to copy
             pages = None if out and part else self._take(1 if part else 0)
-            if -(-length // B) > self.width:
-                pages, bad = None, True
-            else:
-                bad = False
+            bad = -(-length // B) > self.width or self._partial_page_gone(before[0][a], length)
+            if bad:
+                pages = None
             self.tables[c] = [-1] * self.width
             if pages is None:
                 out |= not bad

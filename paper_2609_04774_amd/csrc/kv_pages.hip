@@ -189,10 +189,8 @@ struct ForkList {
     w.seq = c;
     const int len = clamp_len(p.kv_len[a]);
     w.first = len / kBlockTokens;
-    if (pages_of(len) > p.table_stride)
-      w.n = -1;
-    else  // a part of a page to copy, if the parent has that page
-      w.n = len % kBlockTokens != 0 && in_pool(p.tables[a * p.table_stride + w.first], p.n_blocks);
+    const bool part = len % kBlockTokens != 0;  // of a page, to be copied
+    w.n = pages_of(len) > p.table_stride || (part && !in_pool(p.tables[a * p.table_stride + w.first], p.n_blocks)) ? -1 : part;
     w.len = len;
     return w;
   }
@@ -336,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(cp_kv_pool p, CacheSet c
         const int32_t page = from[j];
         to[j] = page;
         if (in_pool(page, p.n_blocks)) atomicAdd(p.refs + page, 1);
-      } else if (j > whole || len % kBlockTokens == 0 || !in_pool(from[whole], p.n_blocks)) {
+      } else if (j > whole || len % kBlockTokens == 0) {
         to[j] = -1;
       }
     }

@@ -320,3 +320,16 @@ def test_tokens_reserved_are_tokens_kept():
             r = slice(9 * s + 8, 9 * s + 9)
             want = owin.attend(f64(q)[r], [8], f64(k)[9 * s:9 * s + 9], f64(v)[9 * s:9 * s + 9], np.arange(9))
             compare(f64(o)[r], f64(lse)[r], want, 9, f"sequence {s}")
+
+
+def test_fork_where_the_last_page_is_gone():
+    """A parent whose last page, filled in part, was given back: there is nothing to
+    copy, so its child gets nothing and is missing.  Pages gone before it, or a length
+    that ends on a page, are shared as they are."""
+    b = Both(9, 8, 40, n_caches=2, seed=13)
+    b.reserve([0, 1, 2, 3], [37, 48, 45, 70])
+    b.free([0, 1, 3], [5, 32, 16], [37, 48, 64])
+    b.fork([0, 1, 2, 3, 0], [4, 5, 6, 7, 8])
+    assert b.missing.tolist() == [2] and b.kv_len.tolist()[4:] == [0, 48, 45, 70, 0]
+    b.reserve([5, 6, 7], [3, 3, 3])                   # what was served can go on
+    assert b.missing.tolist() == [0]
