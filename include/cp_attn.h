@@ -486,10 +486,13 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  * product with the values, and O is divided by the sum of the rounded ones (as in
  * cp_attn_partial): a mean of the values, rounded to bf16.
  * A row that sees no key has O = 0, LSE = -inf; a NaN among its scores gives O =
- * NaN, LSE = -inf.  Keys and values that a row does not see have no effect on
- * it, whatever they hold.  Scores (scaled) may be up to 10^9 in size: far beyond
- * that fp32 no longer holds their differences, and a row may become NaN or count
- * as one that sees no key.
+ * NaN, LSE = -inf.  Keys and values that a row does not see are no part of it,
+ * whatever they hold (an infinity or NaN among them may change the order of its
+ * roundings, and so its last bits).  An infinity or NaN among the values that it does
+ * see makes that element of O infinite or NaN, however small the key's weight.
+ * Scores (scaled) may be up to 10^9 in size: far beyond that fp32 no longer holds
+ * their differences, and a row may become NaN or count as one that sees no key.
+ * Finite values beyond 2^80 may overflow the sums.
  * Errors: CP_ERR_INVALID (shapes, pointers, alignment, scale, window or n_sink < 0),
  * CP_ERR_UNSUPPORTED (head_dim; n_rows above 2^30, or times n_heads_q /
  * n_heads_kv above 2^31 - 1; n_seqs times max_q rows beyond 2^30 blocks),

@@ -399,12 +399,16 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Blocks& block
         if (__builtin_expect(apart(j), 0)) {
           load(j + kAhead);
           if (active) {
+            unsigned keys[NB] = {};  // by the masked scores (by the positions: 384 rows 1 % slower)
+#pragma unroll
+            for (int x = 0; x < 8 * NB; ++x)
+              keys[x / 8] |= (sa[x / 8][x % 8 / 4][x % 4] != -INFINITY ? 1u : 0u) << (x % 8);
 #pragma unroll
             for (int u = 0; u < 12 * NB; ++u) softmax_unit(u, sa, wt, m, sl2);
             finish(wt, l, pf);
 #pragma unroll
             for (int b = 0; b < NB; ++b) mass[b] += weight_sum(pf[b]);
-            pv_not_finite<NB>([&](int db) { return load_v(v_now, fr, db); }, pf, o);
+            pv_not_finite<NB>([&](int db) { return load_v(v_now, fr, db); }, pf, keys, o);
           }
           ++j;
           continue;

@@ -82,14 +82,19 @@ __global__ __launch_bounds__(256) void share_merge_kernel(PagedParams p) {
         for (int i = 0; i < kRows; ++i)
           v[j][i] = reinterpret_cast<const float2*>(slot + (size_t)(r0 + i) * kHeadDim)[lane];
       }
+      float wk[kParts][kRows];
+#pragma unroll
+      for (int j = 0; j < kParts; ++j)
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+          wk[j][i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w[i]), (k + j) & 63));
+      // (A part without keys adds 0 times 0; an infinity or NaN shows whatever its weight.)
 #pragma unroll
       for (int j = 0; j < kParts; ++j)
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-          const float wk = k + j < end ? __shfl(w[i], (k + j) & 63) : 0.f;
-          if (wk == 0.f) continue;  // nothing of a part without keys
-          acc[i].x += wk * v[j][i].x;
-          acc[i].y += wk * v[j][i].y;
+          const float2 a = make_float2(acc[i].x + wk[j][i] * v[j][i].x, acc[i].y + wk[j][i] * v[j][i].y);
+          acc[i] = k + j < end ? a : acc[i];
         }
     }
   }

@@ -375,7 +375,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_rows_kernel(PagedParams 
       // Keys hidden from every row are zeros; hidden from some, they may be anything.
       auto frag = [&](int db) { return v_frag(vt, lane, db); };
       if (__builtin_expect(!open && w.p_lo != w.p_hi && not_finite(frag), 0)) {
-        pv_not_finite<NB>(frag, pf, o);
+        unsigned keys[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) keys[b] = keys_seen(p, t0, g, pos[b]);
+        pv_not_finite<NB>(frag, pf, keys, o);
       } else {
 #pragma unroll
         for (int db = 0; db < 8; ++db) {

@@ -475,12 +475,28 @@ __device__ __forceinline__ bool not_finite(Frag&& v) {
   return __builtin_amdgcn_ballot_w64(bad) != 0;
 }
 
+// The keys of this lane's scores that the row at position pos sees: bit 4 half + r of
+// each.  (A loop: this rare path has to leave registers to the common one.)
+__device__ __forceinline__ unsigned keys_seen(const PagedParams& p, int t0, int g, int pos) {
+  unsigned seen = 0;
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e) {
+    const int key = t0 + 16 * (e >> 2) + 4 * g + (e & 3);
+    const bool sees = key <= pos && key < p.key_end && (!p.window || key > pos - p.window || key < p.n_sink);
+    seen |= (sees ? 1u : 0u) << e;
+  }
+  return seen;
+}
+
 // O^T += V^T P^T of such a tile, where some of its keys are hidden from some rows
 // of the block: a weight of 0 times an infinity would be a NaN.  The finite values
-// are added as ever; a row takes the others from the keys that it sees.
+// are added as ever; a row takes the others from the keys that it sees (as keys_seen
+// gives them), also from those whose weight is 0: so they show in O wherever a tile or a
+// part begins.
 template <int NB, class Frag>
-__device__ __forceinline__ void pv_not_finite(Frag&& v, const bf16x8 (&pf)[NB], f32x4 (&o)[8][NB]) {
-  // (One fragment at a time: this rare path has to leave registers to the common one.)
+__device__ __forceinline__ void pv_not_finite(Frag&& v, const bf16x8 (&pf)[NB], const unsigned (&keys)[NB],
+                                              f32x4 (&o)[8][NB]) {
+  // (One fragment at a time, for the same reason.)
   auto products = [&](auto&& of_value, auto&& use) {
 #pragma unroll
     for (int db = 0; db < 8; ++db) {
@@ -495,7 +511,7 @@ __device__ __forceinline__ void pv_not_finite(Frag&& v, const bf16x8 (&pf)[NB], 
   auto count_seen = [&](int b, const bf16x8& f) {
     bf16x8 seen;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) seen[e] = (__bf16)((float)pf[b][e] == 0.f ? 0.f : 1.f);
+    for (int e = 0; e < 8; ++e) seen[e] = (__bf16)(float)(keys[b] >> e & 1);
     return mfma16(f, seen, f32x4{});
   };
   products([](float x) { return __builtin_isfinite(x) ? x : 0.f; },

@@ -1,5 +1,6 @@
 """GPU checks of what cp_attn_paged and cp_attn_window make of particular values:
-O as a mean of the values with the weights that were used."""
+O as a mean of the values with the weights that were used, and infinite or NaN
+values of keys whose weight is nothing."""
 
 import numpy as np
 import pytest
@@ -111,3 +112,35 @@ def test_mean_of_equal_values_of_a_rank():
         cp.attn_window(plan, q[torch.as_tensor(rows - P, device=DEV)].contiguous(), k, vn, o, ws, window, n_sink=5,
                        k_cache=kc, v_cache=vc, block_table=table)
         assert torch.equal(o, v[torch.arange(Hq) // 4].to(DEV).expand_as(o))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("lens,new,Hq,Hkv,rows", [
+    ([700], [1], 8, 2, None), ([700], [5], 8, 2, None), ([700], [100], 2, 2, 128),
+    ([1400, 1500, 1600, 1550], [512] * 4, 64, 64, 256), ([2048] * 40, [1024] * 40, 16, 1, 384),
+])
+def test_values_of_weight_nothing(lens, new, Hq, Hkv, rows, bad):
+    """A key that a row sees, e^-200 below the others (in fp32 its weight is 0): an
+    infinity or NaN among its values shows in the row, wherever the key lies -- behind
+    other keys or before them, in a tile that every row sees or at the mask's edge, in
+    a part of its own -- and in no row that does not see it."""
+    b = Batch(lens, new, Hq, Hkv, seed=106, uniform=True)
+    b.q.zero_()
+    b.q[:, :, 0] = 1
+    n = new[0]
+    for at in (0, 40, 333, lens[0] - n, lens[0] - n // 2 - 1, lens[0] - 1):
+        for whole in (False, True):  # the key alone, or all those around it
+            for k, v in zip(b.k, b.v):
+                k.zero_()
+                v.fill_(1)
+                k[max(0, at - 100 * whole):at + 1, :, 0] = -200
+                v[at, 0, 3] = bad
+            refill(b)
+            o, _ = run(b, rows, scale=1.0)
+            o = o.view(len(lens), n, Hq, D).float()
+            for s, t in enumerate(lens):
+                sees = torch.arange(t - n, t, device=DEV) >= at
+                shown = ~torch.isfinite(o[s])
+                hit = torch.zeros_like(shown)
+                hit[sees, :Hq // Hkv, 3] = True
+                assert torch.equal(shown, hit), (at, whole, s)
