@@ -459,3 +459,43 @@ def test_append_past_the_table_is_passed_over():
     want = torch.zeros_like(kc)
     want[3, 12:] = 1  # positions 60 .. 63 of sequence 0
     assert torch.equal(kc, want) and torch.equal(vc, want)
+
+
+def test_launches_beside_each_other():
+    """Many launches of single tokens and of chunks queued on two streams, each with its
+    workspace, and page copies on a third, let go together: the results are the bits of
+    the calls by themselves."""
+    a = Batch([30000, 50, 9000, 17000], [1] * 4, 8, 2, seed=93, uniform=True)
+    b = Batch([6000, 900, 3100], [700, 64, 300], 8, 2, seed=94)
+    g = torch.Generator().manual_seed(95)
+    caches = [torch.randint(-99, 99, (2000, B, 2, D), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2)]
+    copied = [c.clone() for c in caches]
+    src = torch.arange(1000, dtype=torch.int32, device=DEV)
+    dst = src + 1000
+    n = 12
+    calls = []
+    for x in (a, b):
+        q = x.q.to(DEV)
+        size = cp.attn_paged_workspace_size(x.kv, len(q), x.max_q, x.Hq)
+        out = [(torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)) for _ in range(n)]
+        calls.append((x, q, torch.empty(size, dtype=torch.uint8, device=DEV), out, x.run()))
+    big = torch.empty(1 << 30, dtype=torch.uint8, device=DEV), torch.empty(1 << 30, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    go = torch.cuda.Event()
+    for _ in range(20):  # some milliseconds, in which the launches queue up
+        big[0].copy_(big[1])
+    go.record()
+    sides = [torch.cuda.Stream() for _ in range(3)]
+    for side in sides:
+        side.wait_event(go)
+    for i in range(n):
+        for side, (x, q, ws, out, _) in zip(sides, calls):
+            cp.attn_paged(x.kv, q, out[i][0], ws, lse=out[i][1], q_start=x.q_start, max_q=x.max_q, stream=side)
+        cp.kv_copy_pages(copied, src, dst, stream=sides[2])
+    torch.cuda.synchronize()
+    for *_, out, want in calls:
+        for o, lse in out:
+            assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    for c, w in zip(copied, caches):
+        w[1000:] = w[:1000]
+        assert torch.equal(c, w)
