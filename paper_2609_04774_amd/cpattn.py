@@ -711,7 +711,7 @@ class KVPool:
         if self.caches.n and self.caches.n_blocks != refs.shape[0]:
             raise ValueError("the caches must hold as many pages as refs")
         self.device = tables.device
-        for name, t in (("kv_len", kv_len), ("refs", refs), ("caches", self.caches.tensors[0] if caches else None)):
+        for name, t in (("kv_len", kv_len), ("refs", refs), ("caches", self.caches.tensors[0] if self.caches.n else None)):
             if t is not None and t.device != self.device:
                 raise ValueError(f"{name} is on {t.device}, tables on {self.device}")
         self.tensors = (tables, kv_len, refs)

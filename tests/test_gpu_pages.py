@@ -333,3 +333,18 @@ def test_fork_where_the_last_page_is_gone():
     assert b.missing.tolist() == [2] and b.kv_len.tolist()[4:] == [0, 48, 45, 70, 0]
     b.reserve([5, 6, 7], [3, 3, 3])                   # what was served can go on
     assert b.missing.tolist() == [0]
+
+
+def test_caches_of_one_tensor():
+    """A pool's caches as the slices of one tensor, or from an iterator."""
+    pair = torch.zeros(2, 12, B, 2, D, dtype=torch.bfloat16, device=DEV)
+    pair[:, 0] = 7
+    tables, kv_len, refs = torch.full((2, 4), -1, dtype=torch.int32, device=DEV), i32([5, 0]), i32([1] + [0] * 11)
+    tables[0, 0] = 0
+    missing = i32([-1])
+    for caches in (pair, iter(pair), iter([])):
+        pool = cp.KVPool(tables, kv_len, refs, caches)
+        cp.kv_fork(pool, i32([0]), i32([1]), missing)
+        assert missing.tolist() == [0] and tables[1].tolist() == [1, -1, -1, -1]
+        cp.kv_free(pool, i32([1]), i32([0]), i32([5]))
+    assert (pair[:, 1] == 7).all()
