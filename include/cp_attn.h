@@ -455,7 +455,9 @@ typedef struct cp_paged_kv {
  * Sizing call of cp_attn_paged (a library utility, not from the paper): device
  * bytes of its workspace for any contents of the device arrays, and for calls of
  * fewer rows; 0 on invalid arguments (cp_last_error says why).  max_q is the
- * call's, without q_start n_rows / n_seqs.
+ * call's, without q_start n_rows / n_seqs.  It is 8.5 MB for up to 16 (row, query
+ * head) pairs per sequence and KV head, 17 for up to 32, else 68 or, from 131072 (row,
+ * query head) pairs of the call on, 101.
  */
 size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_q, int32_t n_heads_q,
                                     int32_t n_heads_kv);
@@ -478,7 +480,8 @@ size_t cp_attn_paged_workspace_size(int32_t n_seqs, int64_t n_rows, int64_t max_
  *   window      keys visible behind a row, itself included; 0: all.
  *   n_sink      first positions that stay visible behind the window, >= 0.
  *   o           bf16 [n_rows][n_heads_q][128].
- *   lse         fp32 [n_rows][n_heads_q], natural log; or NULL.
+ *   lse         fp32 [n_rows][n_heads_q], natural log; or NULL.  Neither output
+ *               may overlap an input.
  *   workspace   device, 256-byte aligned, of the size above; it holds partial
  *               results while the call's kernels run: calls that may overlap
  *               (other streams, graphs replayed side by side) need their own.
@@ -513,7 +516,8 @@ size_t cp_attn_window_workspace_size(const cp_rank_plan* plan, int32_t n_heads_q
  * p attends to the keys j <= p with j > p - window or j < n_sink, of the cached
  * prefix (paged, as in cp_partial_desc) and of the new tokens (all-gathered,
  * original order).  Only the keys that some row sees are read.  (The window
- * itself is not from the paper; window 0 is its causal attention.)
+ * itself is not from the paper; window 0 is its causal attention, which
+ * cp_attn_partial computes faster.)
  *   plan        from cp_shard_plan (checked against it).
  *   q           bf16 [plan->n_rows][n_heads_q][128], local order.
  *   k_new, v_new  bf16 [R][n_heads_kv][128].

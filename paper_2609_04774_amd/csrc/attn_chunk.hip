@@ -16,15 +16,16 @@
 // tile (2 to 3 % of a long launch; added up by vector instructions 6 to 14 %, by
 // 4 x 4 x 4 products 3 to 5 %).
 //
-// Measured (32 query and 8 KV heads): 4096 rows after 32768 tokens (2.34 TFLOP) 1839 us,
-// 1270 TFLOP/s, where a product of two 8192 x 8192 matrices runs at 1210; 256 rows to a
-// block 1961.  A tile takes 0.61 us of 128 rows, 0.93 of 256 and 1.28 of 384, and larger
-// blocks pad more and have fewer walks to share out: alone, 4096 rows take 195 us in
-// blocks of 384 and 173 in those of 256; 200 rows 24 of 256 and 20 of 128; 63 single tokens
-// after 256 to 32768 keys and a chunk of 2048 590 and 520.  So the lengths choose.  One
+// Measured (calls, 32 query and 8 KV heads): 4096 rows after 32768 tokens (2.34 TFLOP) 1923
+// us, 1215 TFLOP/s, where a product of two 8192 x 8192 matrices runs at 1210; 256 rows to
+// a block 2012.  A tile takes 0.63 us of 128 rows, 0.92 of 256 and 1.30 of 384, and larger
+// blocks pad more and have fewer walks to share out: alone, 4096 rows take 200 us in
+// blocks of 384 and 175 in those of 256; 200 rows 27.6 of 256 and 20.8 of 128; 63 single
+// tokens after 256 to 32768 keys and a chunk of 2048 605 and 520.  So the lengths choose,
+// within 1 % of the better (3 % for 2048 rows after 32768, which are not offered 384).  One
 // kernel holds the bodies of 128 and 256; with that of 384 its registers were spilled,
 // which is a second kernel that the first may leave the work to.  A rank's 8192 rows
-// through a window of 4096 440 us (0.41 TFLOP), 21 of them the merge.  One barrier for
+// through a window of 4096 436 us (0.41 TFLOP), 22 of them the merge.  One barrier for
 // two tiles against one each: 5 % faster.  KV heads one after another, blocks inside,
 // against the reverse: 4 to 7 %.
 #include <hip/hip_runtime.h>
@@ -42,7 +43,7 @@ constexpr int kBufs = 8;   // LDS buffers of K and of V; tile t uses buffer t % 
 constexpr int kAhead = 5;  // iteration j loads tile j + kAhead
 constexpr int kSetup = 10;  // of a walk, in tiles
 constexpr int kSnap = 4;   // tiles: a part costs its set-up, and its rows a merge
-// A tile of 128, 256 and 384 rows takes 21/32, 1 and 11/8 of 0.93 us.  A share of larger
+// A tile of 128, 256 and 384 rows takes about 21/32, 1 and 11/8 of 0.92 us.  A share of larger
 // blocks costs more besides, in tiles: its set-ups and its parts' merge are larger, and
 // so are, at both edges of a window, the tiles that some row sees in part.
 constexpr int kNarrowSteps = 5;

@@ -53,9 +53,10 @@ int shares_of(int block_rows) { return block_rows == kChunkRows[0] ? kChunkShare
 
 // Ways to cut the rows into blocks, of which the lengths choose.  The widest blocks
 // are worth a second kernel's launch (4 us where it has nothing to do) to calls of many
-// rows only.  One prompt's 4096 rows of 32 and 8 heads with and without
-// the choice: alone 203 and 204 us, after 8K tokens 654 and 684, after 32K 1839 and 1961;
-// 2048 rows alone 84 and 80, after 8K 315 and 316, after 32K 978 and 1016.
+// rows only.  One prompt's 4096 rows of 32 and 8 heads with and without the choice:
+// alone 177 and 175 us, after 8K tokens 614 and 639, after 32K 1923 and 2032.  Of 2048 rows
+// blocks of 384 alone take 99 us, the others as chosen 81; after 8K 306 and 305, after 32K
+// 973 and 1006.
 int ways_of(int block_rows, int64_t n_rows, int32_t Hq) {
   return block_rows != kChunkRows[0] ? 1 : n_rows * Hq >= 131072 ? 3 : 2;
 }
@@ -76,8 +77,8 @@ Blocks cut(const PagedParams& p, int rows) {
   const int64_t places = (int64_t)p.n_segments * b.n;
   // Blocks of a share, where each has several; not where most places have no rows
   // (few long chunks among many sequences: those places are passed over in order).
-  // Against the order of the blocks themselves: rank 0 of a 32K prompt at degree 4
-  // 1977 us, 2132; through a window of 4096 433, 459.
+  // Against the order of the blocks themselves (before the sums of rounded weights): rank
+  // 0 of a 32K prompt at degree 4 1977 us, 2132; through a window of 4096 433, 459.
   const int64_t full = p.n_rows * p.G / rows;
   const int64_t run = places * p.Hkv / p.n_shares;
   b.run = rows >= kChunkRows[0] && run > 1 && 2 * full >= places ? (int32_t)run : 1;

@@ -24,9 +24,10 @@
 // Long walks over a pool that the Infinity Cache (256 MB) cannot hold stream (loads with
 // the non-temporal hint), but for pages that another sequence of the batch names too
 // (a shared prefix).  64 sequences of 8192 keys 338 us against 370 with plain loads; of
-// one prefix of 8192 keys 117, of 32768 keys for 32 sequences 225 (streamed, 346).  Walks of
+// one prefix of 8192 keys 117 to 126, of 32768 keys for 32 sequences 225 (streamed, 346).  Walks of
 // fewer keys than 1280 do not: at 300 they take 246 us plain and 278 streamed, at 1024
-// 229 and 233, at 1536 226 and 222, at 4096 230 and 215 (1.2 GB each).
+// 229 and 233, at 1536 226 and 222, at 4096 230 and 215 (1.2 GB each).  Sequences past the
+// 512th, or whose first page is gone, find no other: their long walks stream.
 //
 // Measured (32 query and 8 KV heads): 64 sequences of 8192 keys 338 us, 6.35 TB/s, where
 // a plain read of as much runs at 6.0 to 6.5.  One sequence of 4101 keys 19 us, of which

@@ -9,10 +9,13 @@
 // counts 8192 at a time, so that which page a sequence gets never depends on
 // timing.
 //
-// Measured: 20.7K rows of 8 heads appended 27 us, 6.3 TB/s, 64 rows 2.9; 64 sequences
+// Measured: 20.7K rows of 8 heads appended 28 us, 6.1 TB/s, 64 rows 3.1; 64 sequences
 // forked off 8, with 56 pages copied in 8 caches, 13 us to find the pages and 8 for the
-// tables and copies; 128 sequences' pages freed 4.7; 1000 pages of 8 caches moved, 526 MB,
-// 8 us for the list and 95 for the moves, 5.5 TB/s.
+// tables and copies; 128 sequences' pages freed 4.8; 1000 pages of 8 caches moved, 526 MB,
+// 8 us for the list and 96 for the moves, 5.5 TB/s.  A token of 64 sequences reserved 6 to
+// 8 us where no page is needed; where all need one and all but the last 2048 pages are in
+// use, 14 of a pool of 4096 pages, 28 of 32768 and 85 of 131072: the search passes over the
+// pages in use, 8192 in about 5 us.
 #include <hip/hip_runtime.h>
 
 #include "paged.h"
