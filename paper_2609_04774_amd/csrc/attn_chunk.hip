@@ -22,12 +22,13 @@
 // blocks pad more and have fewer walks to share out: alone, 4096 rows take 200 us in
 // blocks of 384 and 175 in those of 256; 200 rows 27.6 of 256 and 20.8 of 128; 63 single
 // tokens after 256 to 32768 keys and a chunk of 2048 605 and 520.  So the lengths choose,
-// within 1 % of the better (3 % for 2048 rows after 32768, which are not offered 384).  One
-// kernel holds the bodies of 128 and 256; with that of 384 its registers were spilled,
-// which is a second kernel that the first may leave the work to.  A rank's 8192 rows
-// through a window of 4096 436 us (0.41 TFLOP), 22 of them the merge.  One barrier for
-// two tiles against one each: 5 % faster.  KV heads one after another, blocks inside,
-// against the reverse: 4 to 7 %.
+// within 1 % of a kernel of the better size alone (200 rows 21.7, as both ways are counted;
+// 2048 rows after 32768 1006 and 973, as they are not offered 384).  One kernel holds the
+// bodies of 128 and 256; with that of 384 its registers were spilled, which is a second
+// kernel that the first may leave the work to.  A rank's 8192 rows through a window of
+// 4096 436 us (0.41 TFLOP), 22 of them the merge.  One barrier for two tiles against one
+// each: 5 % faster.  KV heads one after another, blocks inside, against the reverse: 4 to
+// 7 %.
 #include <hip/hip_runtime.h>
 
 #include "attn_tile.h"
